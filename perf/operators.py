@@ -186,7 +186,7 @@ def _dequantized(q, scale, group):
 def _quantize8(x, group):
     """8-bit integers and their scales: s = max|x| / 127 in 32 bits, q = x / s rounded to the nearest integer, ties to even.
     The quotient is taken in 64 bits: many inputs lie next to a border (half of a group's largest value does)."""
-    s = _group_amax(x, group) / 127.0
+    s = (_group_amax(x, group).double() / 127).to(torch.float32)
     wide = _spread(s, group, x.shape[1]).double()
     q = torch.where(wide > 0, torch.round(x.double() / wide), torch.zeros_like(wide))
     return q.to(torch.int8), s
