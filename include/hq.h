@@ -316,6 +316,90 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
                        const int64_t* latency, int64_t size_limit, int64_t bops_limit, int64_t latency_limit,
                        int32_t* choice_out, int64_t* objective_out);
 
+/* =====================================================================================================
+ * Layers with floating-point activations: 4-bit weights with a scale per group of inputs, and activations
+ * saved in 8 bits for a backward pass.
+ *
+ * The calls above are the integer-only pipeline; these stand beside it for language models, whose activations
+ * stay in 16 bits, and for tuning them.  The weights are packed as everywhere here (signed, two per byte along
+ * the inputs, input 2j in bits 3:0 of byte j) and have no zero point; their scales are floating-point numbers.
+ * Sums are held in 32 bits and rounded once, to the type of the output.
+ *
+ *   - matrices are row-major with a stride between rows; `data` and the quantized arrays are 16-byte aligned
+ *     (HQ_ERR_ALIGNMENT), scales and biases aligned to their type;
+ *   - every call runs on the device of its handle, whatever the current one; `stream` belongs to that device;
+ *   - input and output of a call must not overlap; rows x cols of a matrix may pass 2^31, neither of them may
+ *     (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;
+ *   - no call allocates or needs scratch memory: calls through one handle may run on several streams at once,
+ *     and can be captured into graphs;
+ *   - infinities and NaN go through the arithmetic as IEEE has them.
+ * ===================================================================================================== */
+typedef enum { HQ_F32 = 0, HQ_F16 = 1, HQ_BF16 = 2 } hq_float_type;
+
+typedef struct {      /* matrix of floating-point values */
+  void* data;         /* device pointer, caller-owned */
+  int64_t rows, cols;
+  int64_t row_stride; /* values from one row to the next, >= cols */
+  int32_t type;       /* hq_float_type */
+} hq_matrix;
+
+typedef struct {      /* 4-bit weights: w[i][j] = q[i][j] * scale[i][j / group] */
+  const void* q;      /* [n][k / 2] bytes, dense */
+  const void* scale;  /* [n][ceil(k / group)], dense, of the activations' type */
+  int32_t n, k;       /* outputs and inputs of the layer; k even */
+  int32_t group;      /* inputs per scale: a multiple of 32 (>= k: one scale per output) */
+} hq_w4;
+
+typedef struct {      /* activations saved in 8 bits: value = q * scale */
+  int8_t* q;          /* [rows][cols], dense */
+  float* scale;       /* [rows][ceil(cols / group)], dense */
+  int64_t rows, cols;
+  int32_t group;      /* columns per scale: 32, 64, 128 or 256 */
+} hq_saved8;
+
+typedef enum {
+  HQ_ACT_NONE = 0,    /* f(x) = x */
+  HQ_ACT_RELU = 1,    /* max(x, 0) */
+  HQ_ACT_GELU = 2,    /* x Phi(x), Phi the normal distribution function */
+  HQ_ACT_SILU = 3     /* x / (1 + exp(-x)) */
+} hq_activation;
+
+/*
+ * Linear layer:  out[m][i] = bias[i] + sum_j x[m][j] * w[i][j].
+ * x: (m, k), out: (m, n), both HQ_F16 or HQ_BF16 and of one type; bias: n values of that type or NULL.  Up to 16 rows
+ * (one token of each of a few sequences) the weights' integers enter the products and a group's sum is scaled in
+ * 32 bits; beyond, each w[i][j] is first rounded to the type of x, as a 16-bit weight matrix would hold it.
+ */
+hq_status hq_linear_w4(hq_handle* h, const hq_matrix* x, const hq_w4* w, const void* bias, hq_matrix* out, void* stream);
+
+/* Gradient of hq_linear_w4 with respect to its input:  dx[m][j] = sum_i dy[m][i] * w[i][j].  dy: (m, n), dx: (m, k), types
+ * and the rounding of w as above, for any number of rows. */
+hq_status hq_linear_w4_dgrad(hq_handle* h, const hq_matrix* dy, const hq_w4* w, hq_matrix* dx, void* stream);
+
+/*
+ * Activation that saves its input for the backward pass:  y = f(x), or y = f(x) * gate;
+ *   scale = max|x| / 127 over a group of a row (rounded to 32 bits),  q = x / scale rounded to the nearest integer, ties
+ *   to even, of the exact quotient; a group of zeros has scale 0 and q = 0.  A group that holds an infinity or a NaN has
+ *   scale NaN and q = 0: all of it is restored as NaN.
+ * x, gate, y: (rows, cols) of one type, HQ_F32, HQ_F16 or HQ_BF16.  gate (and with it saved_gate) may be NULL, y may be NULL
+ * (x is saved and nothing else).
+ */
+hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, int32_t act, hq_matrix* y,
+                       hq_saved8* saved_x, hq_saved8* saved_gate, void* stream);
+
+/* Backward pass of hq_act_save8 from what it saved, x^ and gate^ the restored values:
+ *   dx = dy * f'(x^), or dx = dy * gate^ * f'(x^) and dgate = dy * f(x^).   f' of ReLU is 0 at 0.
+ * dy, dx, dgate: (rows, cols) of one type.  saved_gate and dgate are both given or both NULL. */
+hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act,
+                           hq_matrix* dx, hq_matrix* dgate, void* stream);
+
+/*
+ * Gradient of a weight matrix whose input was saved in 8 bits:  dw[i][j] = sum_m dy[m][i] * q[m][j] * scale[m][j / group].
+ * dy: (m, n), dw: (n, k), both HQ_F16 or HQ_BF16 and of one type; saved: (m, k).  Each restored value is rounded to the type
+ * of dy before the products.  m == 0 writes zeros.
+ */
+hq_status hq_linear_wgrad8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved, hq_matrix* dw, void* stream);
+
 const char* hq_status_string(hq_status s);
 
 #ifdef __cplusplus

@@ -25,7 +25,9 @@ EXPORTS = [
     "hq_network_destroy", "hq_set_conv_path", "hq_set_tile_order", "hq_status_string", "hq_network_time_layers", "hq_conv2d_noalloc", "hq_expire_wait_selftest",
     "hq_network_check_guards", "hq_conv2d_noalloc_sync", "hq_mma_peak_launch",
     "hq_ilp_solve", "hq_concat_requant", "hq_sumpool", "hq_conv2d_plan",
+    "hq_linear_w4", "hq_linear_w4_dgrad", "hq_act_save8", "hq_act_backward8", "hq_linear_wgrad8",
 ]
+HQ_ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 class HqError(RuntimeError):
@@ -64,6 +66,18 @@ class hq_layer(C.Structure):
                 ("pool_stride", C.c_int32), ("pool_pad", C.c_int32), ("out_bits", C.c_int32),
                 ("out_signed", C.c_int32), ("relu", C.c_int32), ("qmin", C.c_int32), ("qmax", C.c_int32),
                 ("n_in", C.c_int32), ("ins", C.c_int32 * 8), ("rescales", hq_dyadic * 8)]
+
+
+class hq_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64), ("type", C.c_int32)]
+
+
+class hq_w4(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("n", C.c_int32), ("k", C.c_int32), ("group", C.c_int32)]
+
+
+class hq_saved8(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("group", C.c_int32)]
 
 
 _lib = None
@@ -105,6 +119,13 @@ def lib():
         L.hq_expire_wait_selftest.restype = i32
         i64p = C.POINTER(C.c_int64)
         L.hq_ilp_solve.argtypes = [i32, i64p, i64p, i64p, i64p, C.c_int64, C.c_int64, C.c_int64, C.POINTER(i32), i64p]
+        # the operators on floating-point activations take their structures as byte strings (see _packed_matrix)
+        st = C.c_char_p
+        L.hq_linear_w4.argtypes = [vp, st, st, vp, st, vp]
+        L.hq_linear_w4_dgrad.argtypes = [vp, st, st, st, vp]
+        L.hq_act_save8.argtypes = [vp, st, st, i32, st, st, st, vp]
+        L.hq_act_backward8.argtypes = [vp, st, st, st, i32, st, st, vp]
+        L.hq_linear_wgrad8.argtypes = [vp, st, st, st, vp]
         L.hq_status_string.argtypes = [i32]
         L.hq_status_string.restype = C.c_char_p
         for name in EXPORTS:
@@ -157,6 +178,7 @@ def _check(code: int, where: str):
 
 
 _raw_stream = None
+_raw_stream_of = None
 
 
 def _stream():
@@ -201,6 +223,40 @@ def _wrapped_conv(*v) -> bytes:
     """hq_conv_desc through ctypes: seven integers, seven pointers (w, bias, b, c, residual, rb, rc), relu, qmin, qmax."""
     res = C.cast(C.c_void_p(v[11]), C.POINTER(hq_tensor))
     return bytes(hq_conv_desc(*v[:9], hq_dyadic(*v[9:11]), res, hq_dyadic(*v[12:14]), *v[14:]))
+
+
+# hq_matrix, hq_w4 and hq_saved8 as byte strings.
+_PACK_MATRIX = struct.Struct("@P3qi4x").pack
+_PACK_W4 = struct.Struct("@2P3i4x").pack
+_PACK_SAVED8 = struct.Struct("@2P2qi4x").pack
+_FLOAT_TYPES: dict = {}
+
+
+def _float_type(dtype) -> int:
+    """hq_float_type of a torch dtype; -1, which the library refuses, for any other."""
+    if not _FLOAT_TYPES:
+        import torch
+        _FLOAT_TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return _FLOAT_TYPES.get(dtype, -1)
+
+
+def _packed_matrix(t, device: int) -> bytes:
+    """Describe a two-dimensional CUDA tensor with contiguous rows as an hq_matrix."""
+    rows, cols = t.shape
+    row_stride, col_stride = t.stride()
+    if t.get_device() != device or (col_stride != 1 and cols > 1):
+        raise ValueError("a matrix of this call is on another device, or its rows are not contiguous")
+    return _PACK_MATRIX(t.data_ptr(), rows, cols, row_stride if rows > 1 else max(cols, 1), _float_type(t.dtype))
+
+
+def _grouped(q, scale, group: int, columns: int, itemsize: int, device: int):
+    """Check a quantized matrix with a scale per `group` columns: dense tensors of matching shapes on the device."""
+    rows = q.shape[0]
+    if group < 1 or q.dim() != 2 or q.element_size() != 1 or tuple(scale.shape) != (rows, (columns + group - 1) // group) or scale.element_size() != itemsize:
+        raise ValueError("quantized values and scales do not match: one scale per group of columns and row")
+    if not (q.is_contiguous() and scale.is_contiguous()) or q.get_device() != device or scale.get_device() != device:
+        raise ValueError("quantized values and scales have to be dense and on the handle's device")
+    return rows
 
 
 def to_device(a):
@@ -250,6 +306,7 @@ class Handle:
 
     def __init__(self, device: int = 0):
         self._h = C.c_void_p()
+        self.device = device
         _check(lib().hq_create(device, C.byref(self._h)), "hq_create")
 
     def close(self):
@@ -325,6 +382,64 @@ class Handle:
         ti = tensor_of(x, ch, bits, signed)
         to = tensor_of(out, ch, bits, signed)
         return lib().hq_maxpool(self._h, C.byref(ti), k, stride, pad, C.byref(to), _stream())
+
+    # ---- floating-point activations: 4-bit weights with group scales, activations saved in 8 bits ------------------------
+    # Tensors are two-dimensional with contiguous rows; the quantized ones and their scales are dense.  The calls run on the
+    # current stream of the handle's device.
+    def _device_stream(self) -> int:
+        global _raw_stream_of
+        if _raw_stream_of is None:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _raw_stream_of = raw if raw else (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream_of(self.device)
+
+    def _w4(self, q, scale, group: int, dtype) -> bytes:
+        n = _grouped(q, scale, group, 2 * q.shape[1], 2, self.device)
+        if scale.dtype != dtype:
+            raise ValueError("the scales have to be of the activations' type")
+        return _PACK_W4(q.data_ptr(), scale.data_ptr(), n, 2 * q.shape[1], group)
+
+    def _saved8(self, q, scale, group: int) -> bytes:
+        import torch
+        rows = _grouped(q, scale, group, q.shape[1], 4, self.device)
+        if q.dtype != torch.int8 or scale.dtype != torch.float32:
+            raise ValueError("saved activations are int8 with float32 scales")
+        return _PACK_SAVED8(q.data_ptr(), scale.data_ptr(), rows, q.shape[1], group)
+
+    def linear_w4(self, x, q, scale, group: int, bias, out):
+        """out (m, n) = x (m, k) W^T + bias; q: (n, k / 2) bytes, scale: (n, ceil(k / group)), bias: (n,) or None, all of x's type."""
+        if bias is not None and (bias.dtype != x.dtype or tuple(bias.shape) != (q.shape[0],) or not bias.is_contiguous()
+                                 or bias.get_device() != self.device):
+            raise ValueError("the bias is a dense vector of n values of the activations' type on the handle's device")
+        d = self.device
+        return lib().hq_linear_w4(self._h, _packed_matrix(x, d), self._w4(q, scale, group, x.dtype),
+                                  bias.data_ptr() if bias is not None else None, _packed_matrix(out, d), self._device_stream())
+
+    def linear_w4_dgrad(self, dy, q, scale, group: int, dx):
+        """dx (m, k) = dy (m, n) W."""
+        d = self.device
+        return lib().hq_linear_w4_dgrad(self._h, _packed_matrix(dy, d), self._w4(q, scale, group, dy.dtype), _packed_matrix(dx, d),
+                                        self._device_stream())
+
+    def act_save8(self, x, gate, act: str, group: int, y, xq, xs, gq=None, gs=None):
+        """y = f(x) [* gate]; (xq, xs) and, with a gate, (gq, gs) receive what the backward pass needs.  y may be None."""
+        d = self.device
+        return lib().hq_act_save8(self._h, _packed_matrix(x, d), _packed_matrix(gate, d) if gate is not None else None,
+                                  HQ_ACTIVATION.get(act, -1), _packed_matrix(y, d) if y is not None else None, self._saved8(xq, xs, group),
+                                  self._saved8(gq, gs, group) if gq is not None else None, self._device_stream())
+
+    def act_backward8(self, dy, xq, xs, gq, gs, act: str, group: int, dx, dgate=None):
+        """dx = dy f'(x^) [* gate^] and, with a gate, dgate = dy f(x^), from what act_save8 wrote."""
+        d = self.device
+        return lib().hq_act_backward8(self._h, _packed_matrix(dy, d), self._saved8(xq, xs, group),
+                                      self._saved8(gq, gs, group) if gq is not None else None, HQ_ACTIVATION.get(act, -1),
+                                      _packed_matrix(dx, d), _packed_matrix(dgate, d) if dgate is not None else None, self._device_stream())
+
+    def linear_wgrad8(self, dy, xq, xs, group: int, dw):
+        """dw (n, k) = dy^T (m, n) times the activations (m, k) saved in (xq, xs)."""
+        d = self.device
+        return lib().hq_linear_wgrad8(self._h, _packed_matrix(dy, d), self._saved8(xq, xs, group), _packed_matrix(dw, d), self._device_stream())
 
     # ---- convenience for the dict-shaped single-layer cases of the workload generator -------
     def conv_case(self, case: dict, dev: dict | None = None, out=None):

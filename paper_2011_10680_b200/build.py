@@ -11,7 +11,8 @@ import subprocess
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-CSRC = os.path.join(HERE, "csrc")
+CSRC = os.path.join(HERE, "csrc")                  # the integer-only inference pipeline: no floating point
+CSRC_FLOAT = os.path.join(HERE, "csrc_float")      # the operators on floating-point activations
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libhq.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -19,11 +20,11 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def sources() -> list[str]:
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.cu"))) + sorted(glob.glob(os.path.join(CSRC_FLOAT, "*.cu")))
 
 
 def headers() -> list[str]:
-    return glob.glob(os.path.join(CSRC, "*.cuh")) + [os.path.join(HERE, "..", "include", "hq.h")]
+    return glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC_FLOAT, "*.cuh")) + [os.path.join(HERE, "..", "include", "hq.h")]
 
 
 def _obj(src: str) -> str:

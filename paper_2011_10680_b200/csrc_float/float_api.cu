@@ -1,0 +1,162 @@
+// C ABI of the operators on floating-point activations: argument checks and the choice of kernel.  Host code only.
+#include "float_internal.cuh"
+
+namespace {
+
+constexpr long long kMaxExtent = 0x7fffffffll - 1024;     // 32-bit indexes of a tile may reach past the last row or column
+
+// The handle's device for the duration of a call.
+class DeviceScope {
+ public:
+  explicit DeviceScope(int device) {
+    ok_ = cudaGetDevice(&before_) == cudaSuccess && (before_ == device || cudaSetDevice(device) == cudaSuccess);
+    changed_ = ok_ && before_ != device;
+  }
+  ~DeviceScope() { if (changed_) cudaSetDevice(before_); }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+  bool ok() const { return ok_; }
+
+ private:
+  int before_ = 0;
+  bool ok_ = false, changed_ = false;
+};
+
+inline bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+hq_status check_matrix(const hq_matrix* m, bool f32) {
+  if (!m) return HQ_ERR_INVALID_ARG;
+  if (!(m->type == HQ_F16 || m->type == HQ_BF16 || (m->type == HQ_F32 && f32))) return HQ_ERR_INVALID_ARG;
+  if (m->rows < 0 || m->cols < 1 || m->row_stride < m->cols) return HQ_ERR_INVALID_ARG;
+  if (m->rows > kMaxExtent || m->cols > kMaxExtent || m->row_stride > (1ll << 40)) return HQ_ERR_UNSUPPORTED;
+  if (m->rows > 0 && !m->data) return HQ_ERR_INVALID_ARG;
+  return aligned(m->data, 16) ? HQ_OK : HQ_ERR_ALIGNMENT;
+}
+inline bool same_shape(const hq_matrix* a, const hq_matrix* b) { return a->rows == b->rows && a->cols == b->cols && a->type == b->type; }
+
+hq_status check_w4(const hq_w4* w) {
+  if (!w || !w->q || !w->scale) return HQ_ERR_INVALID_ARG;
+  if (w->n < 1 || w->k < 2 || (w->k & 1) || w->group < 32 || w->group % 32) return HQ_ERR_INVALID_ARG;
+  if (w->n > kMaxExtent || w->k > kMaxExtent) return HQ_ERR_UNSUPPORTED;
+  return aligned(w->q, 16) && aligned(w->scale, 2) ? HQ_OK : HQ_ERR_ALIGNMENT;
+}
+
+hq_status check_saved(const hq_saved8* s, long long rows, long long cols) {
+  if (!s || s->rows != rows || s->cols != cols) return HQ_ERR_INVALID_ARG;
+  if (!(s->group == 32 || s->group == 64 || s->group == 128 || s->group == 256)) return HQ_ERR_INVALID_ARG;
+  if (rows > 0 && (!s->q || !s->scale)) return HQ_ERR_INVALID_ARG;
+  return aligned(s->q, 16) && aligned(s->scale, 4) ? HQ_OK : HQ_ERR_ALIGNMENT;
+}
+
+inline int groups_of(long long cols, int group) { return (int)((cols + group - 1) / group); }
+
+hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
+  const DeviceScope device(h->device);
+  if (!device.ok()) return HQ_ERR_CUDA;
+  return hq_launch_product_any(kind, type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+
+// What hq_act_save8 and hq_act_backward8 share.
+hq_status act_args(const hq_matrix* shape, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act, ActArgs& a) {
+  if (act < HQ_ACT_NONE || act > HQ_ACT_SILU) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_saved(saved_x, shape->rows, shape->cols);
+  if (st != HQ_OK) return st;
+  if (saved_gate) {
+    st = check_saved(saved_gate, shape->rows, shape->cols);
+    if (st != HQ_OK) return st;
+    if (saved_gate->group != saved_x->group) return HQ_ERR_INVALID_ARG;
+    a.gq = saved_gate->q; a.gs = saved_gate->scale;
+  }
+  a.xq = saved_x->q; a.xs = saved_x->scale;
+  a.rows = shape->rows; a.cols = (int32_t)shape->cols; a.group = saved_x->group; a.groups = groups_of(shape->cols, saved_x->group);
+  a.act = act;
+  return HQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hq_status hq_linear_w4(hq_handle* h, const hq_matrix* x, const hq_w4* w, const void* bias, hq_matrix* out, void* stream) {
+  if (!h) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_w4(w);
+  if (st == HQ_OK) st = check_matrix(x, false);
+  if (st == HQ_OK) st = check_matrix(out, false);
+  if (st != HQ_OK) return st;
+  if (x->type != out->type || x->rows != out->rows || x->cols != w->k || out->cols != w->n) return HQ_ERR_INVALID_ARG;
+  if (!aligned(bias, 2)) return HQ_ERR_ALIGNMENT;
+  if (x->rows == 0) return HQ_OK;
+  ProductArgs a{};
+  a.q = w->q; a.scale = w->scale; a.q_cols = w->k; a.groups = groups_of(w->k, w->group); a.group = w->group;
+  a.b = x->data; a.b_stride = x->row_stride; a.bias = bias; a.out = out->data; a.out_stride = out->row_stride;
+  a.i = w->n; a.j = (int32_t)x->rows; a.r = w->k;
+  return product(h, PRODUCT_FORWARD, x->type, a, stream);
+}
+
+hq_status hq_linear_w4_dgrad(hq_handle* h, const hq_matrix* dy, const hq_w4* w, hq_matrix* dx, void* stream) {
+  if (!h) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_w4(w);
+  if (st == HQ_OK) st = check_matrix(dy, false);
+  if (st == HQ_OK) st = check_matrix(dx, false);
+  if (st != HQ_OK) return st;
+  if (dy->type != dx->type || dy->rows != dx->rows || dy->cols != w->n || dx->cols != w->k) return HQ_ERR_INVALID_ARG;
+  if (dy->rows == 0) return HQ_OK;
+  ProductArgs a{};
+  a.q = w->q; a.scale = w->scale; a.q_cols = w->k; a.groups = groups_of(w->k, w->group); a.group = w->group;
+  a.b = dy->data; a.b_stride = dy->row_stride; a.out = dx->data; a.out_stride = dx->row_stride;
+  a.i = w->k; a.j = (int32_t)dy->rows; a.r = w->n;
+  return product(h, PRODUCT_DGRAD, dy->type, a, stream);
+}
+
+hq_status hq_linear_wgrad8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved, hq_matrix* dw, void* stream) {
+  if (!h) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_matrix(dy, false);
+  if (st == HQ_OK) st = check_matrix(dw, false);
+  if (st == HQ_OK) st = check_saved(saved, dy->rows, dw->cols);
+  if (st != HQ_OK) return st;
+  if (dw->type != dy->type || dw->rows != dy->cols) return HQ_ERR_INVALID_ARG;
+  ProductArgs a{};
+  a.q = saved->q; a.scale = saved->scale; a.q_cols = (int32_t)saved->cols; a.groups = groups_of(saved->cols, saved->group); a.group = saved->group;
+  a.b = dy->data; a.b_stride = dy->row_stride; a.out = dw->data; a.out_stride = dw->row_stride;
+  a.i = (int32_t)dw->cols; a.j = (int32_t)dw->rows; a.r = (int32_t)dy->rows;
+  return product(h, PRODUCT_WGRAD, dy->type, a, stream);
+}
+
+hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, int32_t act, hq_matrix* y,
+                       hq_saved8* saved_x, hq_saved8* saved_gate, void* stream) {
+  if (!h || !saved_x || (gate != nullptr) != (saved_gate != nullptr)) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_matrix(x, true);
+  if (st == HQ_OK && gate) st = check_matrix(gate, true);
+  if (st == HQ_OK && y) st = check_matrix(y, true);
+  if (st != HQ_OK) return st;
+  if ((gate && !same_shape(x, gate)) || (y && !same_shape(x, y))) return HQ_ERR_INVALID_ARG;
+  ActArgs a{};
+  st = act_args(x, saved_x, saved_gate, act, a);
+  if (st != HQ_OK || x->rows == 0) return st;
+  a.x = x->data; a.x_stride = x->row_stride;
+  if (gate) { a.gate = gate->data; a.gate_stride = gate->row_stride; }
+  if (y) { a.y = y->data; a.y_stride = y->row_stride; }
+  const DeviceScope device(h->device);
+  if (!device.ok()) return HQ_ERR_CUDA;
+  return hq_launch_act_save8(x->type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+
+hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act,
+                           hq_matrix* dx, hq_matrix* dgate, void* stream) {
+  if (!h || !saved_x || !dx || (dgate != nullptr) != (saved_gate != nullptr)) return HQ_ERR_INVALID_ARG;
+  hq_status st = check_matrix(dy, true);
+  if (st == HQ_OK) st = check_matrix(dx, true);
+  if (st == HQ_OK && dgate) st = check_matrix(dgate, true);
+  if (st != HQ_OK) return st;
+  if (!same_shape(dy, dx) || (dgate && !same_shape(dy, dgate))) return HQ_ERR_INVALID_ARG;
+  ActArgs a{};
+  st = act_args(dy, saved_x, saved_gate, act, a);
+  if (st != HQ_OK || dy->rows == 0) return st;
+  a.x = dy->data; a.x_stride = dy->row_stride; a.y = dx->data; a.y_stride = dx->row_stride;
+  if (dgate) { a.dgate = dgate->data; a.dgate_stride = dgate->row_stride; }
+  const DeviceScope device(h->device);
+  if (!device.ok()) return HQ_ERR_CUDA;
+  return hq_launch_act_backward8(dy->type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+}
+
+}  // extern "C"

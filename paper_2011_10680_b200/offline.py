@@ -7,6 +7,7 @@ Nothing in this module is called while a layer runs.
 
     fold_bn            conv weights + batch-norm statistics -> folded weights and bias          (Appendix D)
     quantize_weights   symmetric, per output channel, k bits                                    (Appendix A)
+    quantize_weights_grouped   4 bits with a scale per group of inputs, for hq_linear_w4
     quantize_bias      INT32 at scale S_h * S_w[oc], so that it adds to the accumulator         (Section 3.2)
     dyadic_from_scale  DN(.): real scale -> (b, c) with b / 2^c ~= scale                        (Section 3.1)
     conv_params        one layer: the arrays of an hq_conv_desc / a table row
@@ -20,7 +21,7 @@ from __future__ import annotations
 
 import numpy as np
 
-__all__ = ["dyadic_from_scale", "fold_bn", "quantize_weights", "quantize_bias", "conv_params", "quantize_network",
+__all__ = ["dyadic_from_scale", "fold_bn", "quantize_weights", "quantize_weights_grouped", "quantize_bias", "conv_params", "quantize_network",
            "float_forward", "calibrate", "fold_input_zero_point"]
 
 
@@ -78,6 +79,35 @@ def quantize_weights(w: np.ndarray, bits: int):
     s_w = np.where(s_w > 0, s_w, 1.0)                 # an all-zero channel: any scale represents it
     q = np.floor(w / s_w[:, None, None, None] + 0.5)
     return np.clip(q, -wmax, wmax).astype(np.int64), s_w
+
+
+def _to_bf16(v: np.ndarray) -> np.ndarray:
+    """float32 values rounded to the nearest bfloat16 value (ties to even), as float32."""
+    u = np.asarray(v, np.float32).view(np.uint32).astype(np.uint64)
+    return ((u + 0x7fff + ((u >> 16) & 1)) & 0xffff0000).astype(np.uint32).view(np.float32)
+
+
+def quantize_weights_grouped(w: np.ndarray, group: int, scale_type: str = "bf16"):
+    """Symmetric 4-bit quantization of a linear layer's weights [n][k] with a scale per `group` inputs of an output:
+    S = max|w| / 7 over the group, rounded to the type it is kept in ("bf16" or "fp16"), q = Int(w / S) in [-7, 7].
+    Returns (q int64 [n][k], S float32 [n][ceil(k / group)]); pack4 packs q."""
+    w = np.asarray(w, np.float64)
+    if w.ndim != 2 or group < 1:
+        raise ValueError("a matrix and a positive group are wanted")
+    if not np.all(np.isfinite(w)):
+        raise ValueError("weights have to be finite")
+    n, k = w.shape
+    groups = (k + group - 1) // group
+    padded = np.zeros((n, groups * group))
+    padded[:, :k] = w
+    top = (np.abs(padded).reshape(n, groups, group).max(axis=2) / 7).astype(np.float32)
+    if scale_type == "fp16" and np.any(top > 65504):
+        raise ValueError("a weight is too large for the scales' type")
+    s = {"bf16": _to_bf16, "fp16": lambda v: v.astype(np.float16).astype(np.float32)}[scale_type](top)
+    if not np.all(np.isfinite(s)):
+        raise ValueError("a weight is too large for the scales' type")
+    wide = np.repeat(np.where(s > 0, s, 1.0).astype(np.float64), group, axis=1)[:, :k]     # a group of zeros: any scale represents it
+    return np.clip(np.floor(w / wide + 0.5), -7, 7).astype(np.int64), s
 
 
 def quantize_bias(b_bar: np.ndarray, s_h: float, s_w: np.ndarray) -> np.ndarray:
