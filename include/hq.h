@@ -328,8 +328,8 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
  *   - matrices are row-major with a stride between rows; `data` and the quantized arrays are 16-byte aligned
  *     (HQ_ERR_ALIGNMENT), scales and biases aligned to their type;
  *   - every call runs on the device of its handle, whatever the current one; `stream` belongs to that device;
- *   - input and output of a call must not overlap; rows x cols of a matrix may pass 2^31, neither of them may
- *     (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;
+ *   - input and output of a call must not overlap; rows x cols of a matrix may be as large as memory allows,
+ *     neither of them above 2^30 (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;
  *   - no call allocates or needs scratch memory: calls through one handle may run on several streams at once,
  *     and can be captured into graphs;
  *   - infinities and NaN go through the arithmetic as IEEE has them.

@@ -3,7 +3,7 @@
 
 namespace {
 
-constexpr long long kMaxExtent = 0x7fffffffll - 1024;     // 32-bit indexes of a tile may reach past the last row or column
+constexpr long long kMaxExtent = 1ll << 30;     // 32-bit indexes of a tile or a group may reach past the last row or column
 
 // The handle's device for the duration of a call.
 class DeviceScope {
@@ -53,6 +53,10 @@ inline int groups_of(long long cols, int group) { return (int)((cols + group - 1
 hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
+  if (!(kind == PRODUCT_FORWARD && a.j <= 16) && hq_product_tc_supported(kind, a)) {
+    const hq_status st = hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream);
+    if (st != HQ_ERR_UNSUPPORTED) return st;
+  }
   return hq_launch_product_any(kind, type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
 

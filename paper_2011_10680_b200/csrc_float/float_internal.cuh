@@ -52,6 +52,9 @@ __device__ __forceinline__ int hq_nibble(const uint8_t* row, int col) {
   return (v ^ 8) - 8;
 }
 
+// On the tensor cores (product_tc.cu): every shape whose rows start on 16 bytes.  hq_launch_product_any takes all of them.
+bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a);
+hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
 cudaError_t hq_launch_product_any(ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
 cudaError_t hq_launch_act_save8(int type, const ActArgs& a, cudaStream_t s);
 cudaError_t hq_launch_act_backward8(int type, const ActArgs& a, cudaStream_t s);
