@@ -53,7 +53,8 @@ inline int groups_of(long long cols, int group) { return (int)((cols + group - 1
 hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
-  if (!(kind == PRODUCT_FORWARD && a.j <= 16) && hq_product_tc_supported(kind, a)) {
+  if (kind == PRODUCT_FORWARD && hq_product_few_supported(a)) return hq_launch_product_few(h, type, a, (cudaStream_t)stream);
+  if (hq_product_tc_supported(kind, a)) {
     const hq_status st = hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream);
     if (st != HQ_ERR_UNSUPPORTED) return st;
   }
