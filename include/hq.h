@@ -325,8 +325,8 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
  * the inputs, input 2j in bits 3:0 of byte j) and have no zero point; their scales are floating-point numbers.
  * Sums are held in 32 bits and rounded once, to the type of the output.
  *
- *   - matrices are row-major with a stride between rows; `data` and the quantized arrays are 16-byte aligned
- *     (HQ_ERR_ALIGNMENT), scales and biases aligned to their type;
+ *   - matrices are row-major with a stride between rows; `data`, the quantized arrays and their scales are
+ *     16-byte aligned (HQ_ERR_ALIGNMENT), biases aligned to their type;
  *   - every call runs on the device of its handle, whatever the current one; `stream` belongs to that device;
  *   - input and output of a call must not overlap; rows x cols of a matrix may be as large as memory allows,
  *     neither of them above 2^30 (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;

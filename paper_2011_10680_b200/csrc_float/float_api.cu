@@ -38,14 +38,14 @@ hq_status check_w4(const hq_w4* w) {
   if (!w || !w->q || !w->scale) return HQ_ERR_INVALID_ARG;
   if (w->n < 1 || w->k < 2 || (w->k & 1) || w->group < 32 || w->group % 32) return HQ_ERR_INVALID_ARG;
   if (w->n > kMaxExtent || w->k > kMaxExtent) return HQ_ERR_UNSUPPORTED;
-  return aligned(w->q, 16) && aligned(w->scale, 2) ? HQ_OK : HQ_ERR_ALIGNMENT;
+  return aligned(w->q, 16) && aligned(w->scale, 16) ? HQ_OK : HQ_ERR_ALIGNMENT;
 }
 
 hq_status check_saved(const hq_saved8* s, long long rows, long long cols) {
   if (!s || s->rows != rows || s->cols != cols) return HQ_ERR_INVALID_ARG;
   if (!(s->group == 32 || s->group == 64 || s->group == 128 || s->group == 256)) return HQ_ERR_INVALID_ARG;
   if (rows > 0 && (!s->q || !s->scale)) return HQ_ERR_INVALID_ARG;
-  return aligned(s->q, 16) && aligned(s->scale, 4) ? HQ_OK : HQ_ERR_ALIGNMENT;
+  return aligned(s->q, 16) && aligned(s->scale, 16) ? HQ_OK : HQ_ERR_ALIGNMENT;
 }
 
 inline int groups_of(long long cols, int group) { return (int)((cols + group - 1) / group); }
