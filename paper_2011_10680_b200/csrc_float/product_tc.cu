@@ -1,36 +1,48 @@
 // The three products on the tensor cores (tcgen05.mma kind::f16, 32-bit accumulators in tensor memory):
 //   out[j][i] = bias[i] + sum_r A(i, r) * B(j, r).
 // The quantized operand A lies on the 128 lanes, so that a weight matrix fills them whatever the number of tokens; B lies on
-// NT <= 256 columns.  B comes by TMA as it is stored.  A is converted on its way: eight warps load its integers into registers
-// some steps ahead, restore each value in the type of B - (integer - offset) * scale, one rounding - and write the swizzled tile
-// the MMA reads.  FORWARD tiles are K-major; DGRAD and WGRAD reduce over the rows of what is stored, their tiles are MN-major,
-// so no operand is ever transposed by hand.
-// Roles: one thread fetches B, one issues MMAs, eight warps convert A, four drain the accumulators; CTAs are persistent and have
-// two accumulators, so that a tile is drained while the next one is computed.  When there are too few tiles to go round, the
-// CTAs of a cluster share a tile's reduction and add their parts in rank order through distributed shared memory.
+// NT <= 256 columns.  Both come by TMA as they are stored, A into a ring of its own, from which warps restore each value in the type
+// of B - (integer - offset) * scale, one rounding - and write the swizzled tile the MMA reads.  FORWARD tiles are K-major; DGRAD and
+// WGRAD reduce over the rows of what is stored, their tiles are MN-major, so no operand is ever transposed by hand.
+// Roles: one thread fetches, one issues MMAs, four groups of four warps convert A, each every fourth stage (a stage takes a warp
+// longer than its MMAs take), four warps drain the accumulators; CTAs are persistent and have two accumulators, so that a tile is
+// drained while the next one is computed.  When there are too few tiles to go round, the CTAs of a cluster share a tile's
+// reduction and add their parts in rank order through distributed shared memory.
 #include "../csrc/tc_common.cuh"
 #include "float_internal.cuh"
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 768;
 constexpr int kStep = 64;                         // values of the reduction per stage: 128 bytes, one swizzle span
-constexpr int kConverterWarps = 8;
+constexpr int kGroups = 4;                        // of converter warps, which take the stages in turn: one waits, the other works
+constexpr int kConverterWarps = 4;                // per group
 constexpr int kTileABytes = kTileC * kStep * 2;
 
-enum Role { ROLE_FETCH = 0, ROLE_MMA = 1, ROLE_ALLOC = 2, ROLE_CONVERT = 4, ROLE_DRAIN = 12 };   // by warp
+enum Role { ROLE_FETCH = 0, ROLE_MMA = 1, ROLE_ALLOC = 2, ROLE_CONVERT = 4, ROLE_DRAIN = 20 };   // by warp
 
 template <int NT>
 struct Shape {
-  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : 8;
+  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 5 : 6;
   static constexpr int kStageBytes = kTileABytes + (NT < 64 ? 64 : NT) * kStep * 2;
-  static constexpr int kSharedBytes = kStages * kStageBytes + 1024;
+  static constexpr int kRawBytes = NT == 256 ? 32 * 1024 : 64 * 1024;     // ring of the quantized operand
+  static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
 };
+// One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages; DGRAD 64 rows of 64 bytes and WGRAD 64
+// rows of 128 bytes, one stage.
+template <int KIND>
+struct Unit {
+  static constexpr int kStagesOf = KIND == PRODUCT_FORWARD ? 4 : 1;
+  static constexpr int kRowBytes = KIND == PRODUCT_DGRAD ? 64 : 128, kRows = KIND == PRODUCT_FORWARD ? kTileC : kStep;
+  static constexpr int kBytes = kRowBytes * kRows;
+};
+constexpr int kMaxUnits = 16;
 
 struct Control {
-  unsigned long long full_a[8], full_b[8], empty[8], acc_full[2], acc_empty[2], drain;
+  unsigned long long full_a[8], full_b[8], empty[8], raw_full[kMaxUnits], raw_empty[kMaxUnits], acc_full[2], acc_empty[2], drain;
   uint32_t tmem;
   volatile uint32_t abort_flag;
+  volatile uint32_t flip;
 };
 
 struct TcArgs {
@@ -38,6 +50,7 @@ struct TcArgs {
   int i_tiles, tiles;       // tiles along i; all tiles
   int steps;                // stages of the whole reduction
   int splits, split_steps;  // CTAs per tile, stages of each
+  uint32_t group_mul;       // FORWARD: 2^31 / (group / 32), rounded up, where that divides exactly (see hq_launch_product_tc), else 0
   uint32_t* status;
 };
 
@@ -68,9 +81,9 @@ __device__ __forceinline__ void drain_wait(uint32_t bar, uint32_t parity, uint32
   }
 }
 
-__device__ __forceinline__ uint4 load_stream(const void* p) {
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
   return v;
 }
 __device__ __forceinline__ void store_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -100,13 +113,15 @@ __device__ __forceinline__ uint32_t scaled4(uint32_t magic, uint32_t scale2) {
 }
 // Eight packed 4-bit integers -> eight values times the scale, in order.  The sign bit of each integer is turned over on the way
 // (two's complement to offset by 8).  The subtraction is exact, the product rounds once.
+// (`flip`, Pair<T>::kOffset4, comes out of memory: with both constants of the masking in sight the compiler makes two instructions of
+// each.)
 template <class T>
-__device__ __forceinline__ void convert4(uint32_t w, uint32_t scale2, uint32_t (&out)[4]) {
-  constexpr uint32_t kMask = 0x000f000fu, kFlip = Pair<T>::kMagic4 | 0x00080008u;
-  const uint32_t p0 = scaled4<T>((w & kMask) ^ kFlip, scale2);                 // values 0 and 4
-  const uint32_t p1 = scaled4<T>(((w >> 4) & kMask) ^ kFlip, scale2);          // 1 and 5
-  const uint32_t p2 = scaled4<T>(((w >> 8) & kMask) ^ kFlip, scale2);          // 2 and 6
-  const uint32_t p3 = scaled4<T>(((w >> 12) & kMask) ^ kFlip, scale2);         // 3 and 7
+__device__ __forceinline__ void convert4(uint32_t w, uint32_t scale2, uint32_t flip, uint32_t (&out)[4]) {
+  constexpr uint32_t kMask = 0x000f000fu;
+  const uint32_t p0 = scaled4<T>((w & kMask) ^ flip, scale2);                  // values 0 and 4
+  const uint32_t p1 = scaled4<T>(((w >> 4) & kMask) ^ flip, scale2);           // 1 and 5
+  const uint32_t p2 = scaled4<T>(((w >> 8) & kMask) ^ flip, scale2);           // 2 and 6
+  const uint32_t p3 = scaled4<T>(((w >> 12) & kMask) ^ flip, scale2);          // 3 and 7
   out[0] = __byte_perm(p0, p1, 0x5410);
   out[1] = __byte_perm(p2, p3, 0x5410);
   out[2] = __byte_perm(p0, p1, 0x7632);
@@ -123,110 +138,87 @@ __device__ __forceinline__ void convert8(uint32_t w, float scale, uint32_t& lo, 
   hi = Pair<T>::pack(f[2], f[3]);
 }
 
-// What a converter thread has in flight for one stage: 32 integers of one row, which share a scale.
-template <int KIND> struct Raw { uint4 w[KIND == PRODUCT_WGRAD ? 2 : 1]; float scale; };
-
-// Walks the stages of a CTA's tiles in order and loads this thread's 32 integers of each.
+// The two scales of a converter thread's 64 integers of a stage (one per half), fetched a stage of its group ahead.
 template <int KIND, class T>
-struct Loader {
-  const TcArgs& a;
-  int tile, step, end_step, begin_step;
-  const uint8_t* q;                // of the current stage
-  const uint8_t* scale;
-  int along;                       // FORWARD: first input of the thread's 32; else the row of q
-  int group, group_end;            // FORWARD: scale index and where its group ends
-  bool live;
-  int lane_part, row_part;
+struct Scales {
+  const ProductArgs& p;
+  const int row_part, lane_part;
+  const uint8_t* base;
+  int limit[2];                    // FORWARD: nothing; else 1 if the half's columns exist
+  int second;                      // from the first half's scale to the second's (not FORWARD)
+  bool row_live;
 
-  __device__ __forceinline__ Loader(const TcArgs& args, int t, int first_tile, int begin, int end) : a(args), tile(first_tile), end_step(end), begin_step(begin) {
-    if (KIND == PRODUCT_FORWARD) { row_part = t >> 1; lane_part = (t & 1) * 32; }
-    else { row_part = (t >> 1) & 63; lane_part = (t >> 7) * 64 + (t & 1) * 32; }
-    enter();
-  }
-  __device__ __forceinline__ void enter() {
-    step = begin_step;
-    const ProductArgs& p = a.p;
-    const int i0 = (tile % a.i_tiles) * kTileC;
+  __device__ __forceinline__ Scales(const ProductArgs& args, int t)
+      : p(args), row_part(KIND == PRODUCT_FORWARD ? t : t & 63), lane_part(KIND == PRODUCT_FORWARD ? 0 : (t >> 6) * 64) {}
+  __device__ __forceinline__ void enter(int i0, bool tile_live) {
     if (KIND == PRODUCT_FORWARD) {
       const long long row = i0 + row_part;
-      live = tile < a.tiles && row < p.i;
-      along = begin_step * kStep + lane_part;
-      group = along / p.group;
-      group_end = (group + 1) * p.group;
-      q = (const uint8_t*)p.q + row * (p.q_cols >> 1) + (along >> 1);
-      scale = (const uint8_t*)p.scale + row * p.groups * sizeof(T);
+      row_live = tile_live && row < p.i;
+      base = (const uint8_t*)p.scale + row * p.groups * sizeof(T);
     } else {
       const int col = i0 + lane_part;
-      live = tile < a.tiles && col < p.i;
-      along = begin_step * kStep + row_part;
-      const long long pitch = KIND == PRODUCT_DGRAD ? p.q_cols >> 1 : p.q_cols;
-      q = (const uint8_t*)p.q + along * pitch + (KIND == PRODUCT_DGRAD ? col >> 1 : col);
-      scale = (const uint8_t*)p.scale + ((long long)along * p.groups + col / p.group) * (KIND == PRODUCT_DGRAD ? sizeof(T) : sizeof(float));
+      row_live = tile_live;
+      limit[0] = col < p.i; limit[1] = col + 32 < p.i;
+      second = (col + 32) / p.group - col / p.group;
+      base = (const uint8_t*)p.scale + (long long)(col / p.group) * (KIND == PRODUCT_DGRAD ? sizeof(T) : sizeof(float));
     }
   }
-  __device__ __forceinline__ void load(Raw<KIND>& raw) {
-    const ProductArgs& p = a.p;
-    const bool on = live && along < p.r;
-    raw.scale = 0.f;
-    raw.w[0] = make_uint4(0, 0, 0, 0);
-    if (KIND == PRODUCT_WGRAD) raw.w[KIND == PRODUCT_WGRAD ? 1 : 0] = make_uint4(0, 0, 0, 0);
-    if (on) {
-      raw.w[0] = load_stream(q);
-      if (KIND == PRODUCT_WGRAD) {
-        if (((tile % a.i_tiles) * kTileC + lane_part + 16) < p.i) raw.w[KIND == PRODUCT_WGRAD ? 1 : 0] = load_stream(q + 16);
-        raw.scale = __ldg((const float*)scale);
-      } else if (KIND == PRODUCT_DGRAD) {
-        raw.scale = hq_to_float(*(const T*)scale);
+  // of stage `st` of the tile entered; zero for what does not exist
+  __device__ __forceinline__ void load(int st, uint32_t group_mul, float (&scale)[2]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      scale[h] = 0.f;
+      if (KIND == PRODUCT_FORWARD) {
+        const int k = st * kStep + 32 * h;
+        if (row_live && k < p.r) scale[h] = hq_to_float(((const T*)base)[group_mul ? __umulhi((uint32_t)k >> 4, group_mul) : k / p.group]);
       } else {
-        raw.scale = hq_to_float(((const T*)scale)[group]);
+        const long long row = st * kStep + row_part;
+        if (row_live && row < p.r && limit[h]) {
+          if (KIND == PRODUCT_DGRAD) scale[h] = hq_to_float(((const T*)base)[row * p.groups + h * second]);
+          else scale[h] = ((const float*)base)[row * p.groups + h * second];
+        }
       }
-    }
-    // the next stage
-    if (++step == end_step) { tile += gridDim.x / a.splits; enter(); return; }
-    along += kStep;
-    if (KIND == PRODUCT_FORWARD) {
-      q += kStep / 2;
-      while (along >= group_end) { ++group; group_end += p.group; }
-    } else if (KIND == PRODUCT_DGRAD) {
-      q += (long long)kStep * (p.q_cols >> 1);
-      scale += (long long)kStep * p.groups * sizeof(T);
-    } else {
-      q += (long long)kStep * p.q_cols;
-      scale += (long long)kStep * p.groups * sizeof(float);
     }
   }
 };
 
+// One thread's part of a stage: 64 integers of a row of what was fetched, to one row of the operand tile.
 template <int KIND, class T>
-__device__ __forceinline__ void convert_stage(const Raw<KIND>& raw, uint32_t tile_a, int t) {
-  // row of the tile, and the first of the thread's four 16-byte pieces in it
-  const int row = KIND == PRODUCT_FORWARD ? t >> 1 : (t >> 1) & 63;
-  const uint32_t base = tile_a + (KIND == PRODUCT_FORWARD ? 0 : (t >> 7) * (kStep * 128)) + row * 128;
-  const int piece = (t & 1) * 4;
-  const uint32_t* w = (const uint32_t*)raw.w;
-  const uint32_t scale2 = KIND == PRODUCT_WGRAD ? 0u : Pair<T>::twice(raw.scale);       // exact: the scales have the type T
+__device__ __forceinline__ void convert_stage(uint32_t raw, int stage_of_unit, const float (&scale)[2], uint32_t tile_a, int t, uint32_t flip) {
+  const int row = KIND == PRODUCT_FORWARD ? t : t & 63, half = KIND == PRODUCT_FORWARD ? 0 : t >> 6;
+  const uint32_t to = tile_a + half * (kStep * 128) + row * 128;
+  constexpr int kPieces = KIND == PRODUCT_WGRAD ? 4 : 2;           // of 16 bytes
+  uint4 q[kPieces];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
+  for (int i = 0; i < kPieces; ++i) {
+    const int piece = (KIND == PRODUCT_FORWARD ? stage_of_unit * 2 : half * kPieces) + i;
+    const uint32_t swizzled = KIND == PRODUCT_DGRAD ? piece ^ ((row >> 1) & 3) : piece ^ (row & 7);
+    q[i] = load_shared(raw + row * Unit<KIND>::kRowBytes + (swizzled << 4));
+  }
+  const uint32_t* w = (const uint32_t*)q;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
     uint32_t v[4];
     if (KIND == PRODUCT_WGRAD) {
-      convert8<T>(w[2 * c], raw.scale, v[0], v[1]);
-      convert8<T>(w[2 * c + 1], raw.scale, v[2], v[3]);
+      convert8<T>(w[2 * c], scale[c >> 2], v[0], v[1]);
+      convert8<T>(w[2 * c + 1], scale[c >> 2], v[2], v[3]);
     } else {
-      convert4<T>(w[c], scale2, v);
+      convert4<T>(w[c], Pair<T>::twice(scale[c >> 2]), flip, v);   // (exact: the scales have the type T)
     }
-    store_shared(base + (((piece + c) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
+    store_shared(to + ((c ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
   }
 }
 
 template <int KIND, class T, int NT>
-__global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_constant__ CUtensorMap map_b, const TcArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_b, const TcArgs a) {
   extern __shared__ uint8_t raw_shared[];
   __shared__ Control ctl;
   constexpr int kStages = Shape<NT>::kStages, kStageBytes = Shape<NT>::kStageBytes;
   constexpr int kBoxes = KIND == PRODUCT_WGRAD ? (NT + 63) / 64 : 1;
   constexpr int kBBytes = KIND == PRODUCT_WGRAD ? kBoxes * 64 * kStep * 2 : NT * kStep * 2;     // that a stage's copies bring
   constexpr uint32_t kColumns = NT * 2;
-  const uint32_t base = (smem_u32(raw_shared) + 1023u) & ~1023u;
+  constexpr int kPer = Unit<KIND>::kStagesOf, kUnits = Shape<NT>::kRawBytes / Unit<KIND>::kBytes;
+  const uint32_t base = (smem_u32(raw_shared) + 1023u) & ~1023u, raw_ring = base + kStages * kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const ProductArgs& p = a.p;
   const int rank = a.splits > 1 ? (int)cluster_ctarank() : 0;
@@ -239,9 +231,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       mbar_init(smem_u32(&ctl.full_b[s]), 1);
       mbar_init(smem_u32(&ctl.empty[s]), 1);
     }
+    for (int u = 0; u < kUnits; ++u) { mbar_init(smem_u32(&ctl.raw_full[u]), 1); mbar_init(smem_u32(&ctl.raw_empty[u]), kPer * kConverterWarps); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl.acc_full[b]), 1); mbar_init(smem_u32(&ctl.acc_empty[b]), 4); }
     mbar_init(smem_u32(&ctl.drain), 1);
     ctl.abort_flag = 0;
+    ctl.flip = Pair<T>::kOffset4;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == ROLE_ALLOC) tmem_alloc(smem_u32(&ctl.tmem), kColumns);
@@ -253,12 +247,24 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
 
   if (warp == ROLE_FETCH) {
     if (elect_one()) {
-      int s = 0; uint32_t phase = 0;
+      int s = 0, u = 0;
+      uint32_t phase = 0, u_phase = 0, issued = 0, u_issued = 0;
       bool ok = true;
-      uint32_t issued = 0;
+      // the quantized operand of stages `st` and on
+      auto fetch_unit = [&](int i0, int st) {
+        if (!mbar_wait(smem_u32(&ctl.raw_empty[u]), u_phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER)) return false;
+        const uint32_t bar = smem_u32(&ctl.raw_full[u]), dst = raw_ring + u * Unit<KIND>::kBytes;
+        mbar_expect_tx(bar, Unit<KIND>::kBytes);
+        if (KIND == PRODUCT_FORWARD) tma_load_2d(dst, &map_q, bar, st * (kStep / 2), i0);
+        else tma_load_2d(dst, &map_q, bar, KIND == PRODUCT_DGRAD ? i0 >> 1 : i0, st * kStep);
+        u_issued |= 1u << u;
+        if (++u == kUnits) { u = 0; u_phase ^= 1; }
+        return true;
+      };
       for (int tile = first; tile < a.tiles && ok; tile += stride) {
-        const int j0 = tile / a.i_tiles * NT;
+        const int i0 = tile % a.i_tiles * kTileC, j0 = tile / a.i_tiles * NT;
         for (int st = begin; st < end; ++st) {
+          if ((st - begin) % kPer == 0 && !fetch_unit(i0, st)) { ok = false; break; }
           if (!mbar_wait(smem_u32(&ctl.empty[s]), phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER)) { ok = false; break; }
           const uint32_t bar = smem_u32(&ctl.full_b[s]), dst = base + s * kStageBytes + kTileABytes;
           mbar_expect_tx(bar, kBBytes);
@@ -275,6 +281,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       if (!ok) {                                                 // given up: let the copies in flight land before the memory goes
         for (int k = 0; k < kStages; ++k)
           if (issued >> k & 1) drain_wait(smem_u32(&ctl.full_b[k]), k < s ? phase : phase ^ 1, a.status);
+        for (int k = 0; k < kUnits; ++k)
+          if (u_issued >> k & 1) drain_wait(smem_u32(&ctl.raw_full[k]), k < u ? u_phase : u_phase ^ 1, a.status);
       }
     }
   } else if (warp == ROLE_MMA) {
@@ -313,31 +321,44 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         drain_wait(smem_u32(&ctl.drain), 0, a.status);
       }
     }
-  } else if (warp >= ROLE_CONVERT && warp < ROLE_CONVERT + kConverterWarps) {
-    constexpr int kAhead = KIND == PRODUCT_WGRAD ? 2 : 4;        // stages in registers
-    const int t = threadIdx.x - ROLE_CONVERT * 32;
-    Loader<KIND, T> loader(a, t, first, begin, end);
-    Raw<KIND> raw[kAhead];
-    const int my_tiles = first < a.tiles ? (a.tiles - first + stride - 1) / stride : 0;
-    const long long total = (long long)my_tiles * (end - begin);
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) loader.load(raw[k]);        // (past the last tile nothing is read)
-    int s = 0; uint32_t phase = 0;
+  } else if (warp >= ROLE_CONVERT && warp < ROLE_CONVERT + kGroups * kConverterWarps) {
+    const int group = (warp - ROLE_CONVERT) / kConverterWarps, t = threadIdx.x - (ROLE_CONVERT + group * kConverterWarps) * 32;
+    const uint32_t flip = ctl.flip;
+    // Stages are numbered through the CTA's tiles, a tile filled up to whole units; the group takes every kGroups-th.
+    const int steps = end - begin, padded = (steps + kPer - 1) / kPer * kPer;
+    Scales<KIND, T> scales(p, t);
+    int tile = first, st = group, tile_no = 0;                   // stage of the tile, and how many tiles came before
+    auto settle = [&]() {
+      bool moved = false;
+      while (st >= padded && tile < a.tiles) { st -= padded; tile += stride; ++tile_no; moved = true; }
+      return moved;
+    };
+    settle();
+    scales.enter(tile % a.i_tiles * kTileC, tile < a.tiles);
+    float scale[2];
+    scales.load(begin + st, a.group_mul, scale);
     bool ok = true;
-    for (long long n = 0; n < total && ok; n += kAhead) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (n + k < total && ok) {
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER));
-          if (ok) {
-            convert_stage<KIND, T>(raw[k], base + s * kStageBytes, t);
-            loader.load(raw[k]);
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl.full_a[s]));
-            if (++s == kStages) { s = 0; phase ^= 1; }
-          }
-        }
+    while (tile < a.tiles && ok) {
+      const long long n = (long long)tile_no * steps + st, v = (long long)tile_no * padded + st;
+      const bool real = st < steps;
+      const unsigned unit_no = (unsigned)(v / kPer);
+      const int u = unit_no % kUnits, s = (int)((unsigned)n % kStages), of_unit = (int)(v % kPer);
+      const uint32_t u_phase = (unit_no / kUnits) & 1, phase = ((unsigned)n / kStages) & 1;
+      ok = mbar_wait(smem_u32(&ctl.raw_full[u]), u_phase, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER);
+      if (real) ok = ok && mbar_wait(smem_u32(&ctl.empty[s]), phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (real) {
+        convert_stage<KIND, T>(raw_ring + u * Unit<KIND>::kBytes, of_unit, scale, base + s * kStageBytes, t, flip);
+        fence_async_smem();
+      }
+      st += kGroups;
+      if (settle()) scales.enter(tile % a.i_tiles * kTileC, tile < a.tiles);
+      scales.load(begin + st, a.group_mul, scale);
+      __syncwarp();
+      if (lane == 0) {
+        if (real) mbar_arrive(smem_u32(&ctl.full_a[s]));
+        mbar_arrive(smem_u32(&ctl.raw_empty[u]));
       }
     }
   } else if (warp >= ROLE_DRAIN) {
@@ -411,7 +432,7 @@ bool encode_b_map(CUtensorMap* map, int type, const ProductArgs& a, ProductKind 
 }
 
 template <int KIND, class T, int NT>
-cudaError_t launch(const CUtensorMap& map, const TcArgs& a, int grid, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -420,10 +441,10 @@ cudaError_t launch(const CUtensorMap& map, const TcArgs& a, int grid, cudaStream
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = Shape<NT>::kSharedBytes; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, product_tc_kernel<KIND, T, NT>, map, a);
+  return cudaLaunchKernelEx(&cfg, product_tc_kernel<KIND, T, NT>, map[0], map[1], a);
 }
 template <int KIND, class T>
-cudaError_t launch_width(int nt, const CUtensorMap& map, const TcArgs& a, int grid, cudaStream_t s) {
+cudaError_t launch_width(int nt, const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
   switch (nt) {
     case 32: return launch<KIND, T, 32>(map, a, grid, s);
     case 64: return launch<KIND, T, 64>(map, a, grid, s);
@@ -432,7 +453,7 @@ cudaError_t launch_width(int nt, const CUtensorMap& map, const TcArgs& a, int gr
   }
 }
 template <class T>
-cudaError_t launch_kind(ProductKind kind, int nt, const CUtensorMap& map, const TcArgs& a, int grid, cudaStream_t s) {
+cudaError_t launch_kind(ProductKind kind, int nt, const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
   return kind == PRODUCT_FORWARD ? launch_width<PRODUCT_FORWARD, T>(nt, map, a, grid, s)
        : kind == PRODUCT_DGRAD ? launch_width<PRODUCT_DGRAD, T>(nt, map, a, grid, s) : launch_width<PRODUCT_WGRAD, T>(nt, map, a, grid, s);
 }
@@ -473,8 +494,16 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
   a.split_steps = (a.steps + a.splits - 1) / a.splits;
   while (a.splits > 1 && (a.splits - 1) * a.split_steps >= a.steps) { a.splits /= 2; a.split_steps = (a.steps + a.splits - 1) / a.splits; }
   const int grid = a.splits > 1 ? a.tiles * a.splits : (int)(tiles < h->sm_count ? tiles : h->sm_count);
-  CUtensorMap map;
-  if (!encode_b_map(&map, type, p, kind, nt)) return HQ_ERR_CUDA;
+  // k / group by a multiply-high, exact while (k / 32) (group / 32) < 2^31
+  if (kind == PRODUCT_FORWARD && p.r <= (1 << 20)) {
+    const unsigned group32 = (unsigned)(p.group >= p.r ? 1 << 20 : p.group) / 32;
+    a.group_mul = (uint32_t)(((1ull << 31) + group32 - 1) / group32);
+  }
+  CUtensorMap map[2];
+  const bool bytes = kind == PRODUCT_WGRAD;
+  const int unit_row = kind == PRODUCT_DGRAD ? Unit<PRODUCT_DGRAD>::kRowBytes : 128, unit_rows = kind == PRODUCT_FORWARD ? kTileC : kStep;
+  if (!encode_rows_map(&map[0], p.q, kind == PRODUCT_FORWARD ? p.i : p.r, bytes ? p.q_cols : p.q_cols >> 1, unit_row, unit_rows, swizzle_for(unit_row)) ||
+      !encode_b_map(&map[1], type, p, kind, nt)) return HQ_ERR_CUDA;
   const cudaError_t e = type == HQ_F16 ? launch_kind<__half>(kind, nt, map, a, grid, s) : launch_kind<__nv_bfloat16>(kind, nt, map, a, grid, s);
   return e == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
