@@ -13,21 +13,19 @@
 
 namespace {
 
-constexpr int kThreads = 768;
+constexpr int kThreads = 896;
 constexpr int kStep = 64;                         // values of the reduction per stage: 128 bytes, one swizzle span
-constexpr int kGroups = 4;                        // of converter warps, which take the stages in turn: one waits, the other works
-constexpr int kConverterWarps = 4;                // per group
 constexpr int kTileABytes = kTileC * kStep * 2;
 
-enum Role { ROLE_FETCH = 0, ROLE_MMA = 1, ROLE_ALLOC = 2, ROLE_CONVERT = 4, ROLE_DRAIN = 20 };   // by warp
+// Roles by warp.  A warp's scheduler is its number modulo four, and the threads that fetch and issue MMAs, which every stage waits
+// for, share theirs with no converter: beside four of them each of their few instructions took 14 cycles (48 tokens, 8192 x 8192:
+// SCHED_BEFORE us, so SCHED_AFTER).  Accumulator lanes 32 q .. 32 q + 31 belong to warps 4 n + q.
+enum Role { ROLE_FETCH, ROLE_MMA, ROLE_ALLOC, ROLE_CONVERT, ROLE_DRAIN, ROLE_NONE };
+__device__ __forceinline__ Role role_of(int warp) {
+  if (warp & 3) return warp < 24 ? ROLE_CONVERT : ROLE_DRAIN;
+  return warp == 0 ? ROLE_FETCH : warp == 4 ? ROLE_MMA : warp == 8 ? ROLE_ALLOC : warp == 12 ? ROLE_DRAIN : ROLE_NONE;
+}
 
-template <int NT>
-struct Shape {
-  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 5 : 6;
-  static constexpr int kStageBytes = kTileABytes + (NT < 64 ? 64 : NT) * kStep * 2;
-  static constexpr int kRawBytes = NT == 256 ? 32 * 1024 : 64 * 1024;     // ring of the quantized operand
-  static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
-};
 // One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages; DGRAD 64 rows of 64 bytes and WGRAD 64
 // rows of 128 bytes, one stage.
 template <int KIND>
@@ -36,10 +34,30 @@ struct Unit {
   static constexpr int kRowBytes = KIND == PRODUCT_DGRAD ? 64 : 128, kRows = KIND == PRODUCT_FORWARD ? kTileC : kStep;
   static constexpr int kBytes = kRowBytes * kRows;
 };
-constexpr int kMaxUnits = 16;
+// NT = 256: two CTAs of a cluster (neighbouring SMs) share every MMA (cta_group::2), 256 lanes x 256 columns: each converts its own
+// 128 lanes and fetches half of the columns.  One CTA with 256 columns of its own is bound by its shared memory: per stage (512
+// cycles of MMAs) 48 KB go in and 48 KB out beside what the converters move.
+// Converters work in groups, which take the stages in turn (most of a warp's time on one is waiting): two warps with two rows of 64
+// integers per thread, or four with one.  A group may be one round of a ring ahead of another, not two, since a barrier tells a
+// round from the next one only: no more groups than stages in either ring.
+template <int KIND, int NT>
+struct Shape {
+  static constexpr bool kPair = NT == 256, kWgrad = KIND == PRODUCT_WGRAD;
+  static constexpr int kCtas = kPair ? 2 : 1, kColumnsHere = NT / kCtas;
+  static constexpr int kStages = kWgrad ? (NT >= 128 ? 5 : 6) : NT >= 128 ? 6 : 8;
+  static constexpr int kStageBytes = kTileABytes + (kColumnsHere < 64 ? 64 : kColumnsHere) * kStep * 2;
+  static constexpr int kRawBytes = (kWgrad ? 48 : 32) * 1024;       // ring of the quantized operand
+  static constexpr int kUnits = kRawBytes / Unit<KIND>::kBytes;
+  static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
+  static constexpr int kRowsPerThread = kWgrad ? 1 : 2, kConverterWarps = 4 / kRowsPerThread;
+  static constexpr int kGroups = kWgrad ? 4 : kStages;
+  static_assert(kGroups <= kStages && kGroups <= Unit<KIND>::kStagesOf * kUnits && kGroups * kConverterWarps <= 18 && kUnits <= 8 && kStages <= 8);
+};
+
+constexpr int kMaxUnits = 8;
 
 struct Control {
-  unsigned long long full_a[8], full_b[8], empty[8], raw_full[kMaxUnits], raw_empty[kMaxUnits], acc_full[2], acc_empty[2], drain;
+  unsigned long long full[8], empty[8], raw_full[kMaxUnits], raw_empty[kMaxUnits], acc_full[2], acc_empty[2], drain;
   uint32_t tmem;
   volatile uint32_t abort_flag;
   volatile uint32_t flip;
@@ -60,6 +78,39 @@ __device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+}
+// A pair's load: into this CTA's shared memory, counted on a barrier of the leading CTA (`bar`: cluster address).
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// As mbar_wait, seeing what threads of the other CTA wrote before they arrived.
+__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+template <class Ctl>
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, Ctl* ctl, uint32_t* status, uint32_t code) {
+  if (try_wait_cluster(bar, parity)) return true;
+  const unsigned long long t0 = global_ns();
+  while (!try_wait_cluster(bar, parity)) {
+    if (ctl->abort_flag) return false;
+    if (global_ns() - t0 > kWaitBudgetNs) { ctl->abort_flag = 1; atomicCAS(status, 0u, code); return false; }
+  }
+  return true;
 }
 // Operand tile in 128-byte swizzled rows.  K-major: a row is 64 values of the reduction, eight rows are 1024 bytes.  MN-major: a row
 // is 64 values along the lanes / columns, eight rows (steps of the reduction) are 1024 bytes (stride), the next 64 lanes follow
@@ -90,42 +141,38 @@ __device__ __forceinline__ void store_shared(uint32_t addr, uint32_t a, uint32_t
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// Pairs of 16-bit values.  `kMagic4` with a 4-bit number in its low bits is kOffset - 8 + that number, exactly.
+// Pairs of 16-bit values; see convert4 for the constants (lower half, upper half): the exponent with the sign bits of both nibbles, the
+// factors 1 and 1/8, and what is taken off, 128 + 8 and 16 + 8 (bf16), 1024 + 8 and 128 + 8 (fp16).
 template <class T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
   using Two = __nv_bfloat162;
-  static constexpr uint32_t kMagic4 = 0x43004300u, kOffset4 = 0x43084308u;     // 128, 136
+  static constexpr bool kBf16 = true;
+  static constexpr uint32_t kFlip = 0x43404308u, kFactor = 0x3e003f80u, kOffset = 0xc1c0c308u;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const Two v = __floats2bfloat162_rn(lo, hi); return *(const uint32_t*)&v; }
   static __device__ __forceinline__ uint32_t twice(float s) { return pack(s, s); }
 };
 template <> struct Pair<__half> {
   using Two = __half2;
-  static constexpr uint32_t kMagic4 = 0x64006400u, kOffset4 = 0x64086408u;     // 1024, 1032
+  static constexpr bool kBf16 = false;
+  static constexpr uint32_t kFlip = 0x64406408u, kFactor = 0x30003c00u, kOffset = 0xd840e408u;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { const Two v = __floats2half2_rn(lo, hi); return *(const uint32_t*)&v; }
   static __device__ __forceinline__ uint32_t twice(float s) { return pack(s, s); }
 };
-template <class T>
-__device__ __forceinline__ uint32_t scaled4(uint32_t magic, uint32_t scale2) {
-  using Two = typename Pair<T>::Two;
-  const uint32_t offset = Pair<T>::kOffset4;
-  const Two v = __hmul2(__hsub2(*(const Two*)&magic, *(const Two*)&offset), *(const Two*)&scale2);
-  return *(const uint32_t*)&v;
-}
-// Eight packed 4-bit integers -> eight values times the scale, in order.  The sign bit of each integer is turned over on the way
-// (two's complement to offset by 8).  The subtraction is exact, the product rounds once.
-// (`flip`, Pair<T>::kOffset4, comes out of memory: with both constants of the masking in sight the compiler makes two instructions of
-// each.)
+// Eight packed 4-bit integers -> eight values times the scale, in order.  Each byte goes to both halves of a word, the upper one
+// shifted right by one: its lower nibble lands on bits 0-3 of the lower half, its upper nibble on bits 3-6 of the upper half.  Under
+// the exponent of 128 (bf16; 1024 fp16) they stand for 128 + u and 128 + 8 u, u the integer + 8 (its sign bit turned over on the
+// way); one exact multiply-add takes both to the integer, and the product rounds once.
+// (`flip`, Pair<T>::kFlip, comes out of memory: with both constants of the masking in sight the compiler makes two instructions of it.)
 template <class T>
 __device__ __forceinline__ void convert4(uint32_t w, uint32_t scale2, uint32_t flip, uint32_t (&out)[4]) {
-  constexpr uint32_t kMask = 0x000f000fu;
-  const uint32_t p0 = scaled4<T>((w & kMask) ^ flip, scale2);                  // values 0 and 4
-  const uint32_t p1 = scaled4<T>(((w >> 4) & kMask) ^ flip, scale2);           // 1 and 5
-  const uint32_t p2 = scaled4<T>(((w >> 8) & kMask) ^ flip, scale2);           // 2 and 6
-  const uint32_t p3 = scaled4<T>(((w >> 12) & kMask) ^ flip, scale2);          // 3 and 7
-  out[0] = __byte_perm(p0, p1, 0x5410);
-  out[1] = __byte_perm(p2, p3, 0x5410);
-  out[2] = __byte_perm(p0, p1, 0x7632);
-  out[3] = __byte_perm(p2, p3, 0x7632);
+  using Two = typename Pair<T>::Two;
+  const uint32_t shifted = w >> 1, factor = Pair<T>::kFactor, offset = Pair<T>::kOffset;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = (__byte_perm(w, shifted, 0x0400 + 0x1111 * i) & 0x0078000fu) ^ flip;
+    const Two v = __hmul2(__hfma2(*(const Two*)&m, *(const Two*)&factor, *(const Two*)&offset), *(const Two*)&scale2);
+    out[i] = *(const uint32_t*)&v;
+  }
 }
 // Four signed bytes -> four values times a 32-bit scale, rounded once.  2^23 + (byte + 128) is a float whose last byte is that number.
 template <class T>
@@ -138,55 +185,56 @@ __device__ __forceinline__ void convert8(uint32_t w, float scale, uint32_t& lo, 
   hi = Pair<T>::pack(f[2], f[3]);
 }
 
-// The two scales of a converter thread's 64 integers of a stage (one per half), fetched a stage of its group ahead.
-template <int KIND, class T>
+// The scales of a converter thread's rows of a stage, one per half of a row's 64 integers, fetched a turn of its group ahead.
+template <int KIND, class T, int ROWS>
 struct Scales {
   const ProductArgs& p;
-  const int row_part, lane_part;
+  const int row_part, lane_part;   // first of the rows (the second is 32 further on), and the first lane of the half (not FORWARD)
   const uint8_t* base;
-  int limit[2];                    // FORWARD: nothing; else 1 if the half's columns exist
+  bool exists[2];                  // FORWARD: the row; else the half's columns
   int second;                      // from the first half's scale to the second's (not FORWARD)
-  bool row_live;
 
-  __device__ __forceinline__ Scales(const ProductArgs& args, int t)
-      : p(args), row_part(KIND == PRODUCT_FORWARD ? t : t & 63), lane_part(KIND == PRODUCT_FORWARD ? 0 : (t >> 6) * 64) {}
-  __device__ __forceinline__ void enter(int i0, bool tile_live) {
+  __device__ __forceinline__ Scales(const ProductArgs& args, int row, int half) : p(args), row_part(row), lane_part(half * 64) {}
+  __device__ __forceinline__ void enter(int i0, bool tile_exists) {
     if (KIND == PRODUCT_FORWARD) {
       const long long row = i0 + row_part;
-      row_live = tile_live && row < p.i;
+      exists[0] = tile_exists && row < p.i;
+      exists[1] = tile_exists && row + 32 < p.i;
       base = (const uint8_t*)p.scale + row * p.groups * sizeof(T);
     } else {
       const int col = i0 + lane_part;
-      row_live = tile_live;
-      limit[0] = col < p.i; limit[1] = col + 32 < p.i;
+      exists[0] = tile_exists && col < p.i;
+      exists[1] = tile_exists && col + 32 < p.i;
       second = (col + 32) / p.group - col / p.group;
       base = (const uint8_t*)p.scale + (long long)(col / p.group) * (KIND == PRODUCT_DGRAD ? sizeof(T) : sizeof(float));
     }
   }
-  // of stage `st` of the tile entered; zero for what does not exist
-  __device__ __forceinline__ void load(int st, uint32_t group_mul, float (&scale)[2]) const {
+  // of stage `st` of the tile entered, [row][half]; zero for what does not exist
+  __device__ __forceinline__ void load(int st, uint32_t group_mul, float (&scale)[ROWS][2]) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      scale[h] = 0.f;
-      if (KIND == PRODUCT_FORWARD) {
-        const int k = st * kStep + 32 * h;
-        if (row_live && k < p.r) scale[h] = hq_to_float(((const T*)base)[group_mul ? __umulhi((uint32_t)k >> 4, group_mul) : k / p.group]);
-      } else {
-        const long long row = st * kStep + row_part;
-        if (row_live && row < p.r && limit[h]) {
-          if (KIND == PRODUCT_DGRAD) scale[h] = hq_to_float(((const T*)base)[row * p.groups + h * second]);
-          else scale[h] = ((const float*)base)[row * p.groups + h * second];
+      const int k = st * kStep + 32 * h;
+      const uint32_t g = KIND != PRODUCT_FORWARD ? 0 : group_mul ? __umulhi((uint32_t)k >> 4, group_mul) : (uint32_t)k / (uint32_t)p.group;
+#pragma unroll
+      for (int x = 0; x < ROWS; ++x) {
+        scale[x][h] = 0.f;
+        if (KIND == PRODUCT_FORWARD) {
+          if (exists[x] && k < p.r) scale[x][h] = hq_to_float(((const T*)base)[(long long)x * 32 * p.groups + g]);
+        } else {
+          const long long row = st * kStep + row_part + 32 * x;
+          if (exists[h] && row < p.r) {
+            if (KIND == PRODUCT_DGRAD) scale[x][h] = hq_to_float(((const T*)base)[row * p.groups + h * second]);
+            else scale[x][h] = ((const float*)base)[row * p.groups + h * second];
+          }
         }
       }
     }
   }
 };
 
-// One thread's part of a stage: 64 integers of a row of what was fetched, to one row of the operand tile.
+// 64 integers of a row of what was fetched (`half`: the half of the lanes, not FORWARD), restored ...
 template <int KIND, class T>
-__device__ __forceinline__ void convert_stage(uint32_t raw, int stage_of_unit, const float (&scale)[2], uint32_t tile_a, int t, uint32_t flip) {
-  const int row = KIND == PRODUCT_FORWARD ? t : t & 63, half = KIND == PRODUCT_FORWARD ? 0 : t >> 6;
-  const uint32_t to = tile_a + half * (kStep * 128) + row * 128;
+__device__ __forceinline__ void convert_row(uint32_t raw, int stage_of_unit, const float (&scale)[2], int row, int half, uint32_t flip, uint32_t (&v)[8][4]) {
   constexpr int kPieces = KIND == PRODUCT_WGRAD ? 4 : 2;           // of 16 bytes
   uint4 q[kPieces];
 #pragma unroll
@@ -198,54 +246,68 @@ __device__ __forceinline__ void convert_stage(uint32_t raw, int stage_of_unit, c
   const uint32_t* w = (const uint32_t*)q;
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
-    uint32_t v[4];
     if (KIND == PRODUCT_WGRAD) {
-      convert8<T>(w[2 * c], scale[c >> 2], v[0], v[1]);
-      convert8<T>(w[2 * c + 1], scale[c >> 2], v[2], v[3]);
+      convert8<T>(w[2 * c], scale[c >> 2], v[c][0], v[c][1]);
+      convert8<T>(w[2 * c + 1], scale[c >> 2], v[c][2], v[c][3]);
     } else {
-      convert4<T>(w[c], Pair<T>::twice(scale[c >> 2]), flip, v);   // (exact: the scales have the type T)
+      convert4<T>(w[c], Pair<T>::twice(scale[c >> 2]), flip, v[c]);   // (exact: the scales have the type T)
     }
-    store_shared(to + ((c ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
   }
+}
+// ... and written to a row of the operand tile.
+__device__ __forceinline__ void store_row(uint32_t tile_a, int row, int half, const uint32_t (&v)[8][4]) {
+  const uint32_t to = tile_a + half * (kStep * 128) + row * 128;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) store_shared(to + ((c ^ (row & 7)) << 4), v[c][0], v[c][1], v[c][2], v[c][3]);
 }
 
 template <int KIND, class T, int NT>
 __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_b, const TcArgs a) {
   extern __shared__ uint8_t raw_shared[];
   __shared__ Control ctl;
-  constexpr int kStages = Shape<NT>::kStages, kStageBytes = Shape<NT>::kStageBytes;
-  constexpr int kBoxes = KIND == PRODUCT_WGRAD ? (NT + 63) / 64 : 1;
-  constexpr int kBBytes = KIND == PRODUCT_WGRAD ? kBoxes * 64 * kStep * 2 : NT * kStep * 2;     // that a stage's copies bring
+  constexpr bool kPair = Shape<KIND, NT>::kPair;
+  constexpr int kStages = Shape<KIND, NT>::kStages, kStageBytes = Shape<KIND, NT>::kStageBytes, kGroups = Shape<KIND, NT>::kGroups;
+  constexpr int kCtas = Shape<KIND, NT>::kCtas, kColumnsHere = Shape<KIND, NT>::kColumnsHere;
+  constexpr int kBoxes = KIND == PRODUCT_WGRAD ? (kColumnsHere + 63) / 64 : 1;
+  constexpr int kBBytes = KIND == PRODUCT_WGRAD ? kBoxes * 64 * kStep * 2 : kColumnsHere * kStep * 2;     // that a CTA's copies bring per stage
   constexpr uint32_t kColumns = NT * 2;
-  constexpr int kPer = Unit<KIND>::kStagesOf, kUnits = Shape<NT>::kRawBytes / Unit<KIND>::kBytes;
+  constexpr int kPer = Unit<KIND>::kStagesOf, kUnits = Shape<KIND, NT>::kUnits, kRowsPerThread = Shape<KIND, NT>::kRowsPerThread;
+  constexpr int kConverterWarps = Shape<KIND, NT>::kConverterWarps;
   const uint32_t base = (smem_u32(raw_shared) + 1023u) & ~1023u, raw_ring = base + kStages * kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Role role = role_of(warp);
   const ProductArgs& p = a.p;
-  const int rank = a.splits > 1 ? (int)cluster_ctarank() : 0;
-  const int first = blockIdx.x / a.splits, stride = gridDim.x / a.splits;
+  // the CTAs of a cluster: the parts of a tile's reduction, each by one CTA or a pair
+  const bool clustered = kPair || a.splits > 1;
+  const int cta = clustered ? (int)cluster_ctarank() : 0, rank = cta / kCtas, in_pair = cta % kCtas, leader = cta - in_pair;
+  const int first = blockIdx.x / (a.splits * kCtas), stride = gridDim.x / (a.splits * kCtas);
   const int begin = rank * a.split_steps, end = min(a.steps, begin + a.split_steps);
+  auto i_of = [&](int tile) { return (tile % a.i_tiles * kCtas + in_pair) * kTileC; };
+  auto j_of = [&](int tile) { return tile / a.i_tiles * NT; };
+  // the leading CTA's barrier of that name
+  auto leading = [&](unsigned long long& bar) { return kPair ? in_cta(smem_u32(&bar), leader) : smem_u32(&bar); };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(smem_u32(&ctl.full_a[s]), kConverterWarps);
-      mbar_init(smem_u32(&ctl.full_b[s]), 1);
+      mbar_init(smem_u32(&ctl.full[s]), 1 + kCtas * kConverterWarps);
       mbar_init(smem_u32(&ctl.empty[s]), 1);
     }
     for (int u = 0; u < kUnits; ++u) { mbar_init(smem_u32(&ctl.raw_full[u]), 1); mbar_init(smem_u32(&ctl.raw_empty[u]), kPer * kConverterWarps); }
-    for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl.acc_full[b]), 1); mbar_init(smem_u32(&ctl.acc_empty[b]), 4); }
+    for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl.acc_full[b]), 1); mbar_init(smem_u32(&ctl.acc_empty[b]), 4 * kCtas); }
     mbar_init(smem_u32(&ctl.drain), 1);
     ctl.abort_flag = 0;
-    ctl.flip = Pair<T>::kOffset4;
+    ctl.flip = Pair<T>::kFlip;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == ROLE_ALLOC) tmem_alloc(smem_u32(&ctl.tmem), kColumns);
+  if (role == ROLE_ALLOC) { if constexpr (kPair) tmem_alloc2(smem_u32(&ctl.tmem), kColumns); else tmem_alloc(smem_u32(&ctl.tmem), kColumns); }
   tc_fence_before();
   __syncthreads();
+  if (kPair) cluster_sync_all();                                   // both CTAs' barriers exist before either touches the other's
   tc_fence_after();
   const uint32_t tmem = ctl.tmem;
   hq_pdl_entry();
 
-  if (warp == ROLE_FETCH) {
+  if (role == ROLE_FETCH) {
     if (elect_one()) {
       int s = 0, u = 0;
       uint32_t phase = 0, u_phase = 0, issued = 0, u_issued = 0;
@@ -262,111 +324,128 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         return true;
       };
       for (int tile = first; tile < a.tiles && ok; tile += stride) {
-        const int i0 = tile % a.i_tiles * kTileC, j0 = tile / a.i_tiles * NT;
+        const int i0 = i_of(tile), j0 = j_of(tile) + in_pair * kColumnsHere;
         for (int st = begin; st < end; ++st) {
           if ((st - begin) % kPer == 0 && !fetch_unit(i0, st)) { ok = false; break; }
           if (!mbar_wait(smem_u32(&ctl.empty[s]), phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER)) { ok = false; break; }
-          const uint32_t bar = smem_u32(&ctl.full_b[s]), dst = base + s * kStageBytes + kTileABytes;
-          mbar_expect_tx(bar, kBBytes);
-          if (KIND == PRODUCT_WGRAD) {
+          const uint32_t bar = leading(ctl.full[s]), dst = base + s * kStageBytes + kTileABytes;
+          if (in_pair == 0) mbar_expect_tx(smem_u32(&ctl.full[s]), kCtas * kBBytes);
 #pragma unroll
-            for (int b = 0; b < kBoxes; ++b) tma_load_2d(dst + b * (64 * kStep * 2), &map_b, bar, j0 + b * 64, st * kStep);
-          } else {
-            tma_load_2d(dst, &map_b, bar, st * kStep, j0);
+          for (int b = 0; b < kBoxes; ++b) {
+            const int x = KIND == PRODUCT_WGRAD ? j0 + b * 64 : st * kStep, y = KIND == PRODUCT_WGRAD ? st * kStep : j0;
+            if constexpr (kPair) tma_load_2d_pair(dst + b * (64 * kStep * 2), &map_b, bar, x, y);
+            else tma_load_2d(dst + b * (64 * kStep * 2), &map_b, bar, x, y);
           }
           issued |= 1u << s;
           if (++s == kStages) { s = 0; phase ^= 1; }
         }
       }
+      // The last stages' MMAs are done before this CTA may end: they read its memory, and in a pair the other CTA signals its barriers.
+      for (int k = 0; k < kStages && ok; ++k)
+        if (issued >> k & 1) ok = mbar_wait(smem_u32(&ctl.empty[k]), k < s ? phase : phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_DRAIN);
       if (!ok) {                                                 // given up: let the copies in flight land before the memory goes
-        for (int k = 0; k < kStages; ++k)
-          if (issued >> k & 1) drain_wait(smem_u32(&ctl.full_b[k]), k < s ? phase : phase ^ 1, a.status);
+        // (those of the odd CTA of a pair are counted on the leading one, which waits for them before the closing cluster barrier)
+        for (int k = 0; k < kStages && in_pair == 0; ++k)
+          if (issued >> k & 1) drain_wait(smem_u32(&ctl.full[k]), k < s ? phase : phase ^ 1, a.status);   // (or its budget: a converter may be missing)
         for (int k = 0; k < kUnits; ++k)
           if (u_issued >> k & 1) drain_wait(smem_u32(&ctl.raw_full[k]), k < u ? u_phase : u_phase ^ 1, a.status);
       }
     }
-  } else if (warp == ROLE_MMA) {
-    if (elect_one()) {
+  } else if (role == ROLE_MMA) {
+    if (in_pair == 0 && elect_one()) {
       constexpr bool kAMn = KIND != PRODUCT_FORWARD, kBMn = KIND == PRODUCT_WGRAD;
-      constexpr uint32_t kType = sizeof(typename Pair<T>::Two) == 4 && Pair<T>::kMagic4 == 0x43004300u ? 1u : 0u;    // bf16 : fp16
+      constexpr uint32_t kType = Pair<T>::kBf16 ? 1u : 0u;
       constexpr uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | ((uint32_t)kAMn << 15) | ((uint32_t)kBMn << 16) |
-                                 ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kTileC >> 4) << 24);
+                                 ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kCtas * kTileC >> 4) << 24);
+      // completion of the MMAs issued so far, signalled in this CTA and its partner
+      auto commit = [&](unsigned long long& bar) {
+        if constexpr (kPair) { mma_commit_2cta(in_cta(smem_u32(&bar), leader)); mma_commit_2cta(in_cta(smem_u32(&bar), leader + 1)); }
+        else mma_commit(smem_u32(&bar));
+      };
+      auto wait = [&](unsigned long long& bar, uint32_t parity) {
+        if constexpr (kPair) return mbar_wait_cluster(smem_u32(&bar), parity, &ctl, a.status, HQ_DEV_TIMEOUT_MMA);
+        else return mbar_wait(smem_u32(&bar), parity, &ctl, a.status, HQ_DEV_TIMEOUT_MMA);
+      };
       int s = 0; uint32_t phase = 0;
       int buf = 0; uint32_t acc_phase = 0;
       bool ok = true;
+      const uint64_t desc_a = tile_desc(base, kAMn), desc_b = tile_desc(base + kTileABytes, kBMn);    // (addresses fit: no carry)
       for (int tile = first; tile < a.tiles && ok; tile += stride) {
-        if (!mbar_wait(smem_u32(&ctl.acc_empty[buf]), acc_phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_MMA)) { ok = false; break; }
+        if (!wait(ctl.acc_empty[buf], acc_phase ^ 1)) { ok = false; break; }
         tc_fence_after();
         for (int st = begin; st < end; ++st) {
-          if (!mbar_wait(smem_u32(&ctl.full_b[s]), phase, &ctl, a.status, HQ_DEV_TIMEOUT_MMA) ||
-              !mbar_wait(smem_u32(&ctl.full_a[s]), phase, &ctl, a.status, HQ_DEV_TIMEOUT_MMA)) { ok = false; break; }
+          if (!wait(ctl.full[s], phase)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t tile_a = base + s * kStageBytes;
-          uint64_t da = tile_desc(tile_a, kAMn), db = tile_desc(tile_a + kTileABytes, kBMn);
+          const uint64_t da = desc_a + (uint32_t)(s * (kStageBytes >> 4)), db = desc_b + (uint32_t)(s * (kStageBytes >> 4));
 #pragma unroll
           for (int k = 0; k < kStep / 16; ++k) {
-            mma_f16(tmem + buf * NT, da, db, idesc, (st > begin || k > 0) ? 1u : 0u);
-            da += kAMn ? (16 * 128) >> 4 : 2;
-            db += kBMn ? (16 * 128) >> 4 : 2;
+            const uint64_t ak = da + k * (kAMn ? (16 * 128) >> 4 : 2), bk = db + k * (kBMn ? (16 * 128) >> 4 : 2);
+            const uint32_t more = (st > begin || k > 0) ? 1u : 0u;
+            if constexpr (kPair) mma_f16_pair(tmem + buf * NT, ak, bk, idesc, more); else mma_f16(tmem + buf * NT, ak, bk, idesc, more);
           }
-          mma_commit(smem_u32(&ctl.empty[s]));
+          if (st + 1 == end) commit(ctl.acc_full[buf]);
+          commit(ctl.empty[s]);
           if (++s == kStages) { s = 0; phase ^= 1; }
         }
         if (!ok) break;
-        mma_commit(smem_u32(&ctl.acc_full[buf]));
         if (++buf == 2) { buf = 0; acc_phase ^= 1; }
       }
       if (!ok) {
-        mma_commit(smem_u32(&ctl.drain));
+        if constexpr (kPair) mma_commit_2cta(in_cta(smem_u32(&ctl.drain), leader)); else mma_commit(smem_u32(&ctl.drain));
         drain_wait(smem_u32(&ctl.drain), 0, a.status);
       }
     }
-  } else if (warp >= ROLE_CONVERT && warp < ROLE_CONVERT + kGroups * kConverterWarps) {
-    const int group = (warp - ROLE_CONVERT) / kConverterWarps, t = threadIdx.x - (ROLE_CONVERT + group * kConverterWarps) * 32;
+  } else if (role == ROLE_CONVERT && (warp >> 2) * 3 + (warp & 3) - 1 < kGroups * kConverterWarps) {
+    const int number = (warp >> 2) * 3 + (warp & 3) - 1;          // 0 .. 17
+    const int group = number / kConverterWarps, member = number % kConverterWarps;
+    // (two warps: the halves of the lanes, or 64 rows each; four: halves and 32 rows, or 32 rows)
+    const int row0 = (KIND == PRODUCT_FORWARD ? member * 32 * kRowsPerThread : kRowsPerThread == 2 ? 0 : (member & 1) * 32) + lane;
+    const int half = KIND == PRODUCT_FORWARD ? 0 : kRowsPerThread == 2 ? member : member >> 1;
     const uint32_t flip = ctl.flip;
     // Stages are numbered through the CTA's tiles, a tile filled up to whole units; the group takes every kGroups-th.
     const int steps = end - begin, padded = (steps + kPer - 1) / kPer * kPer;
-    Scales<KIND, T> scales(p, t);
-    int tile = first, st = group, tile_no = 0;                   // stage of the tile, and how many tiles came before
+    int tile = first, st = group;                                // a tile, and a stage of it
+    unsigned before = 0, before_padded = 0;                      // stages in the tiles before
     auto settle = [&]() {
       bool moved = false;
-      while (st >= padded && tile < a.tiles) { st -= padded; tile += stride; ++tile_no; moved = true; }
+      while (st >= padded && tile < a.tiles) { st -= padded; tile += stride; before += steps; before_padded += padded; moved = true; }
       return moved;
     };
+    Scales<KIND, T, kRowsPerThread> scales(p, row0, half);
     settle();
-    scales.enter(tile % a.i_tiles * kTileC, tile < a.tiles);
-    float scale[2];
+    scales.enter(i_of(tile), tile < a.tiles);
+    float scale[kRowsPerThread][2];
     scales.load(begin + st, a.group_mul, scale);
-    bool ok = true;
-    while (tile < a.tiles && ok) {
-      const long long n = (long long)tile_no * steps + st, v = (long long)tile_no * padded + st;
+    while (tile < a.tiles) {
+      const unsigned n = before + st, v = before_padded + st, unit_no = v / kPer;
       const bool real = st < steps;
-      const unsigned unit_no = (unsigned)(v / kPer);
-      const int u = unit_no % kUnits, s = (int)((unsigned)n % kStages), of_unit = (int)(v % kPer);
-      const uint32_t u_phase = (unit_no / kUnits) & 1, phase = ((unsigned)n / kStages) & 1;
-      ok = mbar_wait(smem_u32(&ctl.raw_full[u]), u_phase, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER);
-      if (real) ok = ok && mbar_wait(smem_u32(&ctl.empty[s]), phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
+      const int u = unit_no % kUnits, s = (int)(n % kStages);
+      const uint32_t raw = raw_ring + u * Unit<KIND>::kBytes, to = base + s * kStageBytes;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.raw_full[u]), (unit_no / kUnits) & 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) break;
       if (real) {
-        convert_stage<KIND, T>(raw_ring + u * Unit<KIND>::kBytes, of_unit, scale, base + s * kStageBytes, t, flip);
+        // the first row's values are made before the stage they go to is free
+        uint32_t value[8][4];
+        convert_row<KIND, T>(raw, (int)(v % kPer), scale[0], row0, half, flip, value);
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ((n / kStages) & 1) ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) break;
+        store_row(to, row0, half, value);
+        if (kRowsPerThread == 2) {
+          convert_row<KIND, T>(raw, (int)(v % kPer), scale[kRowsPerThread - 1], row0 + 32, half, flip, value);
+          store_row(to, row0 + 32, half, value);
+        }
         fence_async_smem();
+        __syncwarp();
+        if (lane == 0) { if constexpr (kPair) mbar_arrive_cluster(leading(ctl.full[s])); else mbar_arrive(smem_u32(&ctl.full[s])); }
       }
+      if (lane == 0) mbar_arrive(smem_u32(&ctl.raw_empty[u]));
       st += kGroups;
-      if (settle()) scales.enter(tile % a.i_tiles * kTileC, tile < a.tiles);
-      scales.load(begin + st, a.group_mul, scale);
-      __syncwarp();
-      if (lane == 0) {
-        if (real) mbar_arrive(smem_u32(&ctl.full_a[s]));
-        mbar_arrive(smem_u32(&ctl.raw_empty[u]));
-      }
+      if (settle()) scales.enter(i_of(tile), tile < a.tiles);
+      scales.load(begin + st, a.group_mul, scale);               // (behind the fence, which waits for loads too)
     }
-  } else if (warp >= ROLE_DRAIN) {
+  } else if (role == ROLE_DRAIN) {
     const int quad = warp & 3;
     int buf = 0; uint32_t acc_phase = 0;
     for (int tile = first; tile < a.tiles; tile += stride) {
-      const int i = tile % a.i_tiles * kTileC + quad * 32 + lane;
-      const int j0 = tile / a.i_tiles * NT;
+      const int i = i_of(tile) + quad * 32 + lane, j0 = j_of(tile);
       const float add = (p.bias && i < p.i) ? hq_to_float(((const T*)p.bias)[i]) : 0.f;
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.acc_full[buf]), acc_phase, &ctl, a.status, HQ_DEV_TIMEOUT_EPILOGUE))) break;
       tc_fence_after();
@@ -388,14 +467,14 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl.acc_empty[buf]));
+      if (lane == 0) { if constexpr (kPair) mbar_arrive_cluster(leading(ctl.acc_empty[buf])); else mbar_arrive(smem_u32(&ctl.acc_empty[buf])); }
       if (++buf == 2) { buf = 0; acc_phase ^= 1; }
     }
   }
   __syncwarp();
   if (a.splits > 1) {
     cluster_sync_all();                                          // every part is written
-    const int i0 = first % a.i_tiles * kTileC, j0 = first / a.i_tiles * NT;
+    const int i0 = i_of(first), j0 = j_of(first);
     const int cols = NT / a.splits;                              // columns this CTA adds up (splits divides NT)
     const uint32_t mine = base + rank * cols * kTileC * 4;
     for (int e = threadIdx.x; e < cols * kTileC; e += kThreads) {
@@ -404,18 +483,20 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         float sum = 0.f;
         for (int k = 0; k < a.splits; ++k) {
           float v;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(mine + e * 4, k)));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(mine + e * 4, k * kCtas + in_pair)));
           sum += v;
         }
         if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
         ((T*)p.out)[(long long)j * p.out_stride + i] = hq_from_float<T>(sum);
       }
     }
-    cluster_sync_all();                                          // nobody reads a part any more
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == ROLE_ALLOC) { tc_fence_after(); tmem_dealloc(tmem, kColumns); }
+  // The CTAs of a cluster leave together: nobody reads a part any more, the leading CTA has seen its MMAs complete, its partner has
+  // sent its last arrival.
+  if (clustered) cluster_sync_all();
+  if (role == ROLE_ALLOC) { tc_fence_after(); if constexpr (kPair) tmem_dealloc2(tmem, kColumns); else tmem_dealloc(tmem, kColumns); }
 }
 
 // ---------------------------------------------------------------- host side ------------------
@@ -424,7 +505,7 @@ bool encode_b_map(CUtensorMap* map, int type, const ProductArgs& a, ProductKind 
   const long long stride = rows == 1 ? (cols + 7) / 8 * 8 : a.b_stride;      // (the stride of a single row means nothing)
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {kStep, (cuuint32_t)(kind == PRODUCT_WGRAD ? kStep : nt)};
+  const cuuint32_t box[2] = {kStep, (cuuint32_t)(kind == PRODUCT_WGRAD ? kStep : nt == 256 ? 128 : nt)};
   const cuuint32_t estr[2] = {1, 1};
   return g_encode_tiled(map, type == HQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.b), dims,
                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -437,10 +518,10 @@ cudaError_t launch(const CUtensorMap* map, const TcArgs& a, int grid, cudaStream
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)a.splits; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = (unsigned)(a.splits * Shape<KIND, NT>::kCtas); attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = Shape<NT>::kSharedBytes; cfg.stream = s;
-  cfg.attrs = attr; cfg.numAttrs = a.splits > 1 ? 2 : 1;
+  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = Shape<KIND, NT>::kSharedBytes; cfg.stream = s;
+  cfg.attrs = attr; cfg.numAttrs = a.splits * Shape<KIND, NT>::kCtas > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, product_tc_kernel<KIND, T, NT>, map[0], map[1], a);
 }
 template <int KIND, class T>
@@ -460,7 +541,7 @@ cudaError_t launch_kind(ProductKind kind, int nt, const CUtensorMap* map, const 
 
 template <int KIND, class T, int NT>
 bool allow_shared() {
-  return cudaFuncSetAttribute(product_tc_kernel<KIND, T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<NT>::kSharedBytes) == cudaSuccess;
+  return cudaFuncSetAttribute(product_tc_kernel<KIND, T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, NT>::kSharedBytes) == cudaSuccess;
 }
 template <int KIND, class T>
 bool allow_widths() { return allow_shared<KIND, T, 32>() && allow_shared<KIND, T, 64>() && allow_shared<KIND, T, 128>() && allow_shared<KIND, T, 256>(); }
@@ -483,17 +564,29 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
   TcArgs a{};
   a.p = p;
   a.status = h->dev_status;
-  a.i_tiles = (p.i + kTileC - 1) / kTileC;
   a.steps = (p.r + kStep - 1) / kStep;
-  const int nt = p.j > 128 ? 256 : p.j > 64 ? 128 : p.j > 32 ? 64 : 32;
-  const long long tiles = (long long)a.i_tiles * ((p.j + nt - 1) / nt);
-  if (tiles > 0x3fffffff) return HQ_ERR_UNSUPPORTED;
-  a.tiles = (int)tiles;
-  a.splits = 1;
-  while (a.splits < 8 && tiles * a.splits * 2 <= h->sm_count && a.steps >= a.splits * 2 * 4) a.splits *= 2;
-  a.split_steps = (a.steps + a.splits - 1) / a.splits;
-  while (a.splits > 1 && (a.splits - 1) * a.split_steps >= a.steps) { a.splits /= 2; a.split_steps = (a.steps + a.splits - 1) / a.splits; }
-  const int grid = a.splits > 1 ? a.tiles * a.splits : (int)(tiles < h->sm_count ? tiles : h->sm_count);
+  // Columns per tile and CTAs (or pairs) per tile: what is through first, by the cycles that a stage, a tile and the joining of parts
+  // took (stages of 32 / 64 / 128 / 256 columns: STAGE_CYCLES).
+  int nt = 0;
+  long long best = 0;
+  for (const int width : {32, 64, 128, 256}) {
+    const int ctas = width == 256 ? 2 : 1, stage = width == 256 ? 620 : width == 128 ? 560 : width == 64 ? 450 : 430;
+    const long long i_tiles = (p.i + ctas * kTileC - 1) / (ctas * kTileC), tiles = i_tiles * ((p.j + width - 1) / width);
+    if (tiles > 0x3fffffff) continue;
+    for (int splits = 1; splits * ctas <= 8; splits *= 2) {
+      const int split_steps = (a.steps + splits - 1) / splits;
+      if (splits > 1 && ((splits - 1) * split_steps >= a.steps || split_steps < 4)) break;
+      const long long at_once = h->sm_count / (ctas * splits), rounds = (tiles + at_once - 1) / at_once;
+      if (splits > 1 && rounds > 1) break;
+      const long long cost = rounds * ((long long)split_steps * stage + 1500) + (splits > 1 ? 3000 + 10 * width : 0);
+      if (best && cost >= best) continue;
+      best = cost; nt = width;
+      a.i_tiles = (int)i_tiles; a.tiles = (int)tiles; a.splits = splits; a.split_steps = split_steps;
+    }
+  }
+  if (nt == 0) return HQ_ERR_UNSUPPORTED;
+  const int ctas = nt == 256 ? 2 : 1, at_once = h->sm_count / ctas;
+  const int grid = (a.splits > 1 ? a.tiles * a.splits : a.tiles < at_once ? a.tiles : at_once) * ctas;
   // k / group by a multiply-high, exact while (k / 32) (group / 32) < 2^31
   if (kind == PRODUCT_FORWARD && p.r <= (1 << 20)) {
     const unsigned group32 = (unsigned)(p.group >= p.r ? 1 << 20 : p.group) / 32;
