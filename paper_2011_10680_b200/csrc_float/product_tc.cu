@@ -159,15 +159,22 @@ __device__ __forceinline__ void convert4(uint32_t w, uint32_t scale2, uint32_t f
     out[i] = *(const uint32_t*)&v;
   }
 }
-// Four signed bytes -> four values times a 32-bit scale, rounded once.  2^23 + (byte + 128) is a float whose last byte is that number.
+// Four signed bytes -> four values times a 32-bit scale, rounded once.  2^23 + (byte + 128) is a float whose last byte is that number;
+// the subtraction and the product run on pairs.
 template <class T>
-__device__ __forceinline__ void convert8(uint32_t w, float scale, uint32_t& lo, uint32_t& hi) {
+__device__ __forceinline__ void convert8(uint32_t w, unsigned long long scale2, uint32_t& lo, uint32_t& hi) {
   const uint32_t v = w ^ 0x80808080u;
-  float f[4];
+  uint32_t out[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = (__uint_as_float(__byte_perm(v, 0x4b000000u, 0x7540 + i)) - 8388736.f) * scale;
-  lo = Pair<T>::pack(f[0], f[1]);
-  hi = Pair<T>::pack(f[2], f[3]);
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t a = __byte_perm(v, 0x4b000000u, 0x7540 + 2 * i), b = __byte_perm(v, 0x4b000000u, 0x7541 + 2 * i);
+    unsigned long long f;
+    asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tadd.rn.f32x2 t, t, %3;\n\tmul.rn.f32x2 %0, t, %4;\n\t}"
+        : "=l"(f) : "r"(a), "r"(b), "l"(0xcb000080cb000080ull), "l"(scale2));      // - 8388736 twice
+    out[i] = Pair<T>::pack(__uint_as_float((uint32_t)f), __uint_as_float((uint32_t)(f >> 32)));
+  }
+  lo = out[0];
+  hi = out[1];
 }
 
 // The scales of a converter thread's rows of a stage, one per half of a row's 64 integers, fetched a turn of its group ahead.
@@ -232,8 +239,9 @@ __device__ __forceinline__ void convert_row(uint32_t raw, int stage_of_unit, con
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
     if (KIND == PRODUCT_WGRAD) {
-      convert8<T>(w[2 * c], scale[c >> 2], v[c][0], v[c][1]);
-      convert8<T>(w[2 * c + 1], scale[c >> 2], v[c][2], v[c][3]);
+      const unsigned long long scale2 = (unsigned long long)__float_as_uint(scale[c >> 2]) * 0x100000001ull;
+      convert8<T>(w[2 * c], scale2, v[c][0], v[c][1]);
+      convert8<T>(w[2 * c + 1], scale2, v[c][2], v[c][3]);
     } else {
       convert4<T>(w[c], Pair<T>::twice(scale[c >> 2]), flip, v[c]);   // (exact: the scales have the type T)
     }
@@ -342,32 +350,41 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       constexpr uint32_t kType = Pair<T>::kBf16 ? 1u : 0u;
       constexpr uint32_t idesc = (1u << 4) | (kType << 7) | (kType << 10) | ((uint32_t)kAMn << 15) | ((uint32_t)kBMn << 16) |
                                  ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(kCtas * kTileC >> 4) << 24);
-      // completion of the MMAs issued so far, signalled in this CTA and its partner
-      auto commit = [&](unsigned long long& bar) {
-        if constexpr (kPair) { mma_commit_2cta(in_cta(smem_u32(&bar), leader)); mma_commit_2cta(in_cta(smem_u32(&bar), leader + 1)); }
-        else mma_commit(smem_u32(&bar));
+      // completion of the MMAs issued so far, signalled in this CTA and its partner (addresses of the first barrier of a row)
+      struct Both { uint32_t here, there; };
+      auto both = [&](unsigned long long& bar) {
+        if constexpr (kPair) return Both{in_cta(smem_u32(&bar), leader), in_cta(smem_u32(&bar), leader + 1)};
+        else return Both{smem_u32(&bar), 0u};
       };
-      auto wait = [&](unsigned long long& bar, uint32_t parity) { return mbar_wait(smem_u32(&bar), parity, &ctl, a.status, HQ_DEV_TIMEOUT_MMA); };
+      auto commit = [&](const Both& bar, int k) {
+        if constexpr (kPair) { mma_commit_2cta(bar.here + 8 * k); mma_commit_2cta(bar.there + 8 * k); } else mma_commit(bar.here + 8 * k);
+      };
+      const Both empty = both(ctl.empty[0]), acc_full = both(ctl.acc_full[0]);
+      const uint32_t full = smem_u32(&ctl.full[0]);
       int s = 0; uint32_t phase = 0;
       int buf = 0; uint32_t acc_phase = 0;
       bool ok = true;
       const uint64_t desc_a = tile_desc(base, kAMn), desc_b = tile_desc(base + kTileABytes, kBMn);    // (addresses fit: no carry)
+      // (the next stage's barrier is looked at while the present stage's MMAs are issued: the look alone takes some 200 cycles)
+      bool ready = false;
       for (int tile = first; tile < a.tiles && ok; tile += stride) {
-        if (!wait(ctl.acc_empty[buf], acc_phase ^ 1)) { ok = false; break; }
+        if (!mbar_wait(smem_u32(&ctl.acc_empty[buf]), acc_phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_MMA)) { ok = false; break; }
         tc_fence_after();
         for (int st = begin; st < end; ++st) {
-          if (!wait(ctl.full[s], phase)) { ok = false; break; }
+          if (!ready && !mbar_wait(full + 8 * s, phase, &ctl, a.status, HQ_DEV_TIMEOUT_MMA)) { ok = false; break; }
           tc_fence_after();
           const uint64_t da = desc_a + (uint32_t)(s * (kStageBytes >> 4)), db = desc_b + (uint32_t)(s * (kStageBytes >> 4));
+          const int done = s;
+          if (++s == kStages) { s = 0; phase ^= 1; }
+          ready = mbar_try_wait_for(full + 8 * s, phase, 0);
 #pragma unroll
           for (int k = 0; k < kStep / 16; ++k) {
             const uint64_t ak = da + k * (kAMn ? (16 * 128) >> 4 : 2), bk = db + k * (kBMn ? (16 * 128) >> 4 : 2);
             const uint32_t more = (st > begin || k > 0) ? 1u : 0u;
             if constexpr (kPair) mma_f16_pair(tmem + buf * NT, ak, bk, idesc, more); else mma_f16(tmem + buf * NT, ak, bk, idesc, more);
           }
-          if (st + 1 == end) commit(ctl.acc_full[buf]);
-          commit(ctl.empty[s]);
-          if (++s == kStages) { s = 0; phase ^= 1; }
+          if (st + 1 == end) commit(acc_full, buf);
+          commit(empty, done);
         }
         if (!ok) break;
         if (++buf == 2) { buf = 0; acc_phase ^= 1; }
