@@ -20,11 +20,14 @@ constexpr int kTileABytes = kTileC * kStep * 2;
 // Roles by warp.  A warp's scheduler is its number modulo four, and the threads that fetch and issue MMAs, which every stage waits
 // for, share theirs with no converter: beside four of them each of their few instructions took 14 cycles (48 tokens, 8192 x 8192:
 // SCHED_BEFORE us, so SCHED_AFTER).  Accumulator lanes 32 q .. 32 q + 31 belong to warps 4 n + q.
-enum Role { ROLE_FETCH, ROLE_MMA, ROLE_ALLOC, ROLE_CONVERT, ROLE_DRAIN, ROLE_NONE };
+enum Role { ROLE_FETCH, ROLE_MMA, ROLE_ALLOC, ROLE_CONVERT, ROLE_DRAIN };
 __device__ __forceinline__ Role role_of(int warp) {
   if (warp & 3) return warp < 24 ? ROLE_CONVERT : ROLE_DRAIN;
-  return warp == 0 ? ROLE_FETCH : warp == 4 ? ROLE_MMA : warp == 8 ? ROLE_ALLOC : warp == 12 ? ROLE_DRAIN : ROLE_NONE;
+  return warp == 0 ? ROLE_FETCH : warp == 4 ? ROLE_MMA : warp == 8 ? ROLE_ALLOC : warp == 12 ? ROLE_DRAIN : ROLE_CONVERT;
 }
+// Converter warps by number: first the eighteen on schedulers of their own, then the three beside the issuers.
+constexpr int kMaxConverters = 21;
+__device__ __forceinline__ int converter_number(int warp) { return warp & 3 ? (warp >> 2) * 3 + (warp & 3) - 1 : 18 + (warp >> 2) - 4; }
 
 // One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages; DGRAD 64 rows of 64 bytes and WGRAD 64
 // rows of 128 bytes, one stage.
@@ -50,8 +53,8 @@ struct Shape {
   static constexpr int kUnits = kRawBytes / Unit<KIND>::kBytes;
   static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
   static constexpr int kRowsPerThread = kWgrad ? 1 : 2, kConverterWarps = 4 / kRowsPerThread;
-  static constexpr int kGroups = kWgrad ? 4 : kStages;
-  static_assert(kGroups <= kStages && kGroups <= Unit<KIND>::kStagesOf * kUnits && kGroups * kConverterWarps <= 18 && kUnits <= 8 && kStages <= 8);
+  static constexpr int kGroups = kWgrad ? 5 : kStages;
+  static_assert(kGroups <= kStages && kGroups <= Unit<KIND>::kStagesOf * kUnits && kGroups * kConverterWarps <= kMaxConverters && kUnits <= 8 && kStages <= 8);
 };
 
 constexpr int kMaxUnits = 8;
@@ -394,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         drain_wait(smem_u32(&ctl.drain), 0, a.status);
       }
     }
-  } else if (role == ROLE_CONVERT && (warp >> 2) * 3 + (warp & 3) - 1 < kGroups * kConverterWarps) {
-    const int number = (warp >> 2) * 3 + (warp & 3) - 1;          // 0 .. 17
+  } else if (role == ROLE_CONVERT && converter_number(warp) < kGroups * kConverterWarps) {
+    const int number = converter_number(warp);
     const int group = number / kConverterWarps, member = number % kConverterWarps;
     // (two warps: the halves of the lanes, or 64 rows each; four: halves and 32 rows, or 32 rows)
     const int row0 = (KIND == PRODUCT_FORWARD ? member * 32 * kRowsPerThread : kRowsPerThread == 2 ? 0 : (member & 1) * 32) + lane;
@@ -476,17 +479,30 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
     const int i0 = i_of(first), j0 = j_of(first);
     const int cols = NT / a.splits;                              // columns this CTA adds up (splits divides NT)
     const uint32_t mine = base + rank * cols * kTileC * 4;
-    for (int e = threadIdx.x; e < cols * kTileC; e += kThreads) {
-      const int i = i0 + e % kTileC, j = j0 + rank * cols + e / kTileC;
-      if (i < p.i && j < p.j) {
-        float sum = 0.f;
-        for (int k = 0; k < a.splits; ++k) {
-          float v;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(mine + e * 4, k * kCtas + in_pair)));
-          sum += v;
-        }
-        if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
-        ((T*)p.out)[(long long)j * p.out_stride + i] = hq_from_float<T>(sum);
+    const bool whole = p.out_stride % 4 == 0;                    // four values of a row leave in one store
+    for (int e = threadIdx.x; e < cols * (kTileC / 4); e += kThreads) {
+      const int i = i0 + e % (kTileC / 4) * 4, j = j0 + rank * cols + e / (kTileC / 4);
+      if (i >= p.i || j >= p.j) continue;
+      float4 part[4], sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k0 = 0; k0 < a.splits; k0 += 4) {                 // (a remote load takes long: four on their way)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < a.splits)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part[k].x), "=f"(part[k].y), "=f"(part[k].z), "=f"(part[k].w)
+                         : "r"(in_cta(mine + e * 16, (k0 + k) * kCtas + in_pair)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < a.splits) { sum.x += part[k].x; sum.y += part[k].y; sum.z += part[k].z; sum.w += part[k].w; }
+      }
+      float v[4] = {sum.x, sum.y, sum.z, sum.w};
+      T* out = (T*)p.out + (long long)j * p.out_stride + i;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (p.bias && i + k < p.i) v[k] += hq_to_float(((const T*)p.bias)[i + k]);
+      if (whole && i + 4 <= p.i) {
+        *(uint2*)out = make_uint2(Pair<T>::pack(v[0], v[1]), Pair<T>::pack(v[2], v[3]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (i + k < p.i) out[k] = hq_from_float<T>(v[k]);
       }
     }
   }
