@@ -366,9 +366,10 @@ typedef enum {
 
 /*
  * Linear layer:  out[m][i] = bias[i] + sum_j x[m][j] * w[i][j].
- * x: (m, k), out: (m, n), both HQ_F16 or HQ_BF16 and of one type; bias: n values of that type or NULL.  Up to 16 rows
- * (one token of each of a few sequences) the weights' integers enter the products and a group's sum is scaled in
- * 32 bits; beyond, each w[i][j] is first rounded to the type of x, as a 16-bit weight matrix would hold it.
+ * x: (m, k), out: (m, n), both HQ_F16 or HQ_BF16 and of one type; bias: n values of that type or NULL.  With few rows (one token
+ * of each of a few sequences: up to 16, or 8 / 4 where two / four groups share 128 inputs) the weights' integers enter the
+ * products and a group's sum is scaled in 32 bits; with more, each w[i][j] is first rounded to the type of x, as a 16-bit
+ * weight matrix would hold it.
  */
 hq_status hq_linear_w4(hq_handle* h, const hq_matrix* x, const hq_w4* w, const void* bias, hq_matrix* out, void* stream);
 

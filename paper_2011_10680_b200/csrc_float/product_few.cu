@@ -1,4 +1,4 @@
-// hq_linear_w4 for up to 16 rows: the matrix-vector case, one token of each of a few sequences.  The packed weights are read once
+// hq_linear_w4 for few rows: the matrix-vector case, one token of each of a few sequences.  The packed weights are read once
 // and that is the bound, so everything else has to hide behind their stream: at the memory's rate a scheduler has about 350 cycles
 // for 32 outputs x 128 inputs.
 //   - Every warp has a ring of its own: one lane fetches 32 outputs x 256 inputs by TMA, the warp consumes them, and the lane
@@ -24,11 +24,10 @@
 namespace {
 
 constexpr int kThreads = 512, kWarps = 16, kWarpsLog = 4, kRows = 16, kStep = 128;
-constexpr int kMaxShared = 224 * 1024;
-constexpr int kRedPitch = 20;                 // floats per column of partial sums: 16 outputs, four columns on different banks
+constexpr int kMaxShared = 226 * 1024;
+constexpr int kMaxColumns = 16;               // of the matrix instruction, for all rows: rows times parts
 constexpr int kMaxInputs = 1 << 20;           // see FewArgs::group_mul
 constexpr int kStageInputs = 256;             // per fetch: 128 bytes of a row, one swizzle span
-constexpr int kScalePitch = 20;               // bytes of an output's scales per fetch: up to eight, and what 4-byte copies bring along
 constexpr int kMaxDepth = 4;
 
 struct FewArgs {
@@ -41,6 +40,7 @@ struct FewArgs {
                            // Exact while (k / 32) (group / 32) < 2^31, that is up to kMaxInputs inputs
   int depth;               // stages of a warp's ring
   int pitch;               // bytes of a row of x in shared memory
+  int scale_pitch;         // bytes of an output's scales per fetch: two, four or eight, and what 4-byte copies bring along
   int ring_at, scale_at, fix_at, red_at, sum_at;     // shared memory: rings of weights and scales, corrections, the warps' sums, the CTA's
   uint32_t* status;
 };
@@ -94,7 +94,8 @@ template <class T, int NB, int RT, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_constant__ CUtensorMap map_q, const FewArgs a) {
   extern __shared__ uint8_t raw_shared[];
   __shared__ Control ctl;
-  constexpr int kStageBytes = 16 * RT * 128, kScaleBytes = 16 * RT * kScalePitch;
+  constexpr int kStageBytes = 16 * RT * 128;
+  const uint32_t kScaleBytes = 16 * RT * a.scale_pitch;
   const ProductArgs& p = a.p;
   const uint32_t base = (smem_u32(raw_shared) + 1023u) & ~1023u;
   uint8_t* const shared = raw_shared + (base - smem_u32(raw_shared));
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
     if (lane < 16 * RT && row + lane < p.i && k < p.r) {
       const int first = (int)__umulhi((uint32_t)k >> 4, a.group_mul), last = min(first + 2 * parts - 1, p.groups - 1);
       const long long at = (long long)(row + lane) * p.groups;
-      const uint32_t to = scale_ring + f_slot * kScaleBytes + lane * kScalePitch;
+      const uint32_t to = scale_ring + f_slot * kScaleBytes + lane * a.scale_pitch;
       const long long w0 = (at + first) >> 1, w1 = (at + last) >> 1;
 #pragma unroll
       for (int w = 0; w < (WHOLE ? 2 : 5); ++w) {
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
 #pragma unroll
         for (int h = 0; h < 2 * RT; ++h) {
           const uint32_t in_tile = row_in_8 + 8 * h, row = (uint32_t)tile * (16 * RT) + in_tile;
-          s_at[h] = scale_ring + slot * kScaleBytes + in_tile * kScalePitch + (((row * (uint32_t)p.groups + first) & 1) << 1);
+          s_at[h] = scale_ring + slot * kScaleBytes + in_tile * a.scale_pitch + (((row * (uint32_t)p.groups + first) & 1) << 1);
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -327,55 +328,61 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
       if (ok && n + a.depth < units) fetch();
       if (++slot == a.depth) { slot = 0; phase ^= 1; }
      }
-      // the tile's inputs are through: add up the warps' parts
-      float* mine = (float*)(shared + a.red_at) + warp * (kRedPitch * 8 * NB * RT);
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-          for (int k2 = 0; k2 < 4; ++k2) {
-            mine[((r * NB + nb) * 8 + 2 * t + (k2 & 1)) * kRedPitch + row_in_8 + (k2 >> 1) * 8] = total[r][nb][k2];
-            total[r][nb][k2] = 0.f;
-          }
-        }
-      }
+      // the tile's inputs are through: add up the warps' parts, all outputs at once with one eight of columns, sixteen with two (the
+      // sums of 16 outputs of a column lie together, every other pair of columns turned by eight to spread the banks)
       auto meet = [&]() {
         if (a.along_log == 0) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 << a.along_log) : "memory");
       };
-      meet();
-      const float* sums = (const float*)(shared + a.red_at) + (team << a.along_log) * (kRedPitch * 8 * NB * RT);
-      const int members = 32 << a.along_log, outputs = p.j * (16 * RT);
-      auto output = [&](int e, float sum) {
-        const int row = e / (16 * RT), i = tile * (16 * RT) + (e & (16 * RT - 1));
-        if (i < p.i) {
-          if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
-          ((T*)p.out)[row * p.out_stride + i] = hq_from_float<T>(sum);
-        }
-      };
-      for (int e = kw * 32 + lane; e < outputs; e += members) {
-        const int in_tile = e & (16 * RT - 1), row = e / (16 * RT);
-        const float* part = sums + ((in_tile >> 4) * NB * 8 + (row << parts_log)) * kRedPitch + (in_tile & 15);
-        float sum = 0.f;
-        for (int k2 = 0; k2 < along; ++k2, part += kRedPitch * 8 * NB * RT)
-          for (int q = 0; q < parts; ++q) sum += part[q * kRedPitch];
-        if (a.splits == 1) output(e, sum); else ((float*)(shared + a.sum_at))[e] = sum;
-      }
-      if (a.splits > 1) {
-        cluster_sync_all();
-        for (int e = threadIdx.x + rank * kThreads; e < outputs; e += kThreads * a.splits) {
-          float sum = 0.f;
-          for (int c = 0; c < a.splits; ++c) {
-            float v;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(base + a.sum_at + e * 4, c)));
-            sum += v;
+      constexpr int kHalves = NB == 1 ? RT : 1, kSums = 16 * 8 * NB * kHalves;       // sixteens of outputs, values of a warp
+#pragma unroll
+      for (int r0 = 0; r0 < RT; r0 += kHalves) {
+        float* mine = (float*)(shared + a.red_at) + warp * kSums;
+#pragma unroll
+        for (int r = r0; r < r0 + kHalves; ++r)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+          for (int k2 = 0; k2 < 4; ++k2) {
+            mine[(((r - r0) * NB + nb) * 8 + 2 * t + (k2 & 1)) * 16 + ((row_in_8 + (k2 >> 1) * 8) ^ ((t & 1) << 3))] = total[r][nb][k2];
+            total[r][nb][k2] = 0.f;
           }
-          output(e, sum);
         }
-        cluster_sync_all();
+        meet();
+        const float* sums = (const float*)(shared + a.red_at) + (team << a.along_log) * kSums;
+        const int members = 32 << a.along_log, outputs = p.j * (16 * kHalves);
+        auto output = [&](int e, float sum) {
+          const int row = e / (16 * kHalves), i = tile * (16 * RT) + r0 * 16 + (e & (16 * kHalves - 1));
+          if (i < p.i) {
+            if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
+            ((T*)p.out)[row * p.out_stride + i] = hq_from_float<T>(sum);
+          }
+        };
+        for (int e = kw * 32 + lane; e < outputs; e += members) {
+          float sum = 0.f;
+          for (int k2 = 0; k2 < along; ++k2) {
+            for (int q = 0; q < parts; ++q) {
+              const int col = ((e / (16 * kHalves)) << parts_log) + q + (kHalves == 2 ? (e >> 4 & 1) * 8 : 0);
+              sum += sums[k2 * kSums + col * 16 + ((e & 15) ^ ((col >> 1 & 1) << 3))];
+            }
+          }
+          if (a.splits == 1) output(e, sum); else ((float*)(shared + a.sum_at))[e] = sum;
+        }
+        if (a.splits > 1) {
+          cluster_sync_all();
+          for (int e = threadIdx.x + rank * kThreads; e < outputs; e += kThreads * a.splits) {
+            float sum = 0.f;
+            for (int c = 0; c < a.splits; ++c) {
+              float v;
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(base + a.sum_at + e * 4, c)));
+              sum += v;
+            }
+            output(e, sum);
+          }
+          cluster_sync_all();
+        }
+        meet();                                                    // the sums are read
       }
-      meet();                                                      // the sums are read
     }
   };
   if (by_value) work(std::true_type{}); else work(std::false_type{});
@@ -388,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
   }
 }
 
-int columns_eights(int j, int parts) { const int n = (j * parts + 7) / 8; return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
+int columns_eights(int j, int parts) { return j * parts <= 8 ? 1 : 2; }
 
 // Parts of a 128-input step that can have scales of their own.
 int parts_of(const ProductArgs& a) { return a.group >= a.r || a.group % 128 == 0 ? 1 : a.group % 64 == 0 ? 2 : 4; }
@@ -408,8 +415,7 @@ cudaError_t launch(const CUtensorMap& map, const FewArgs& a, int grid, int share
 template <class T, bool WHOLE>
 cudaError_t launch_shape(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, cudaStream_t s) {
   if (rt == 2) return nb == 1 ? launch<T, 1, 2, WHOLE>(map, a, grid, shared, s) : launch<T, 2, 2, WHOLE>(map, a, grid, shared, s);
-  return nb == 1 ? launch<T, 1, 1, WHOLE>(map, a, grid, shared, s) : nb == 2 ? launch<T, 2, 1, WHOLE>(map, a, grid, shared, s)
-       : nb == 4 ? launch<T, 4, 1, WHOLE>(map, a, grid, shared, s) : launch<T, 8, 1, WHOLE>(map, a, grid, shared, s);
+  return nb == 1 ? launch<T, 1, 1, WHOLE>(map, a, grid, shared, s) : launch<T, 2, 1, WHOLE>(map, a, grid, shared, s);
 }
 template <class T>
 cudaError_t launch_type(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, cudaStream_t s) {
@@ -422,8 +428,7 @@ bool allow_shared() {
 }
 template <class T, bool WHOLE>
 bool allow_shapes() {
-  return allow_shared<T, 1, 1, WHOLE>() && allow_shared<T, 2, 1, WHOLE>() && allow_shared<T, 4, 1, WHOLE>() && allow_shared<T, 8, 1, WHOLE>() &&
-         allow_shared<T, 1, 2, WHOLE>() && allow_shared<T, 2, 2, WHOLE>();
+  return allow_shared<T, 1, 1, WHOLE>() && allow_shared<T, 2, 1, WHOLE>() && allow_shared<T, 1, 2, WHOLE>() && allow_shared<T, 2, 2, WHOLE>();
 }
 template <class T>
 bool allow_type() { return allow_shapes<T, false>() && allow_shapes<T, true>(); }
@@ -442,14 +447,16 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
     const long long inputs = (long long)per * kStageInputs;
     const long long pitch = inputs * 2 + 64;                           // 64 modulo 128: eight lanes' pieces lie on different banks
     const long long x_bytes = (256 + p.j * pitch + 1023) & ~1023ll, fix_bytes = (inputs / kStep * 8 * nb * 8 + 127) & ~127ll;
-    // Sixteen or 32 outputs per tile (32 share what is read of x, if the registers hold two columns' eights at most), and teams of
-    // as many warps as leave the longest warp the least: its stages times the outputs of one.
+    // Sixteen or 32 outputs per tile (32 share what is read of x), and teams of as many warps as leave the longest warp the least: its
+    // stages times the outputs of one.
+    const int scale_pitch = parts == 1 ? 8 : parts == 2 ? 12 : 20;
     long long best = 0;
-    for (int r = nb <= 2 ? 2 : 1; r >= 1; --r) {
+    for (int r = 2; r >= 1; --r) {
       const int tiles = (p.i + 16 * r - 1) / (16 * r);
-      const int red_bytes = kWarps * kRedPitch * 8 * nb * r * (int)sizeof(float), sum_bytes = splits > 1 ? 16 * r * p.j * 4 : 0;
+      const int at_a_time = nb == 1 ? r : 1;
+      const int red_bytes = kWarps * 16 * 8 * nb * at_a_time * (int)sizeof(float), sum_bytes = splits > 1 ? 16 * at_a_time * p.j * 4 : 0;
       const long long rest = 1024 + x_bytes + fix_bytes + red_bytes + sum_bytes;
-      const int stage_bytes = kWarps * 16 * r * 128, scale_bytes = kWarps * 16 * r * kScalePitch;
+      const int stage_bytes = kWarps * 16 * r * 128, scale_bytes = kWarps * 16 * r * scale_pitch;
       int depth = rest < kMaxShared ? (int)((kMaxShared - rest) / (stage_bytes + scale_bytes)) : 0;
       if (depth > kMaxDepth) depth = kMaxDepth;
       if (depth < 1) continue;
@@ -461,7 +468,7 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
         best = cost;
         a.p = p;
         a.depth = depth; a.along_log = log; a.tiles = tiles;
-        a.parts_log = parts == 4 ? 2 : parts - 1; a.splits = splits; a.range = per * kStageInputs; a.pitch = (int)pitch;
+        a.parts_log = parts == 4 ? 2 : parts - 1; a.splits = splits; a.range = per * kStageInputs; a.pitch = (int)pitch; a.scale_pitch = scale_pitch;
         a.ring_at = (int)x_bytes;
         a.scale_at = a.ring_at + depth * stage_bytes;
         a.fix_at = a.scale_at + depth * scale_bytes;
@@ -485,7 +492,7 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
 bool hq_product_few_init() { return load_driver_entry_points() && allow_type<__half>() && allow_type<__nv_bfloat16>(); }
 
 bool hq_product_few_supported(const ProductArgs& p) {
-  if (p.j > 16 || p.q_cols % 32 || (p.b_stride % 8 && p.j > 1)) return false;
+  if (p.j > kMaxColumns || p.j * parts_of(p) > kMaxColumns || p.q_cols % 32 || (p.b_stride % 8 && p.j > 1)) return false;
   FewArgs a{};
   int rt, shared;
   return plan(p, 148, a, rt, shared);
