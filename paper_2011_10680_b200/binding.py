@@ -230,33 +230,39 @@ _PACK_MATRIX = struct.Struct("@P3qi4x").pack
 _PACK_W4 = struct.Struct("@2P3i4x").pack
 _PACK_SAVED8 = struct.Struct("@2P2qi4x").pack
 _FLOAT_TYPES: dict = {}
+_SAVED_TYPES: list = []                      # of the integers and the scales of saved activations
 
 
-def _float_type(dtype) -> int:
-    """hq_float_type of a torch dtype; -1, which the library refuses, for any other."""
+def _float_types() -> dict:
+    """hq_float_type of the torch dtypes that have one; others go to the library as -1, which it refuses."""
     if not _FLOAT_TYPES:
         import torch
         _FLOAT_TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
-    return _FLOAT_TYPES.get(dtype, -1)
+    return _FLOAT_TYPES
 
 
 def _packed_matrix(t, device: int) -> bytes:
-    """Describe a two-dimensional CUDA tensor with contiguous rows as an hq_matrix."""
+    """Describe a two-dimensional CUDA tensor with contiguous rows as an hq_matrix.  (A small call is bound by the host: every
+    question to a tensor takes about 0.1 us.)"""
     rows, cols = t.shape
     row_stride, col_stride = t.stride()
-    if t.get_device() != device or (col_stride != 1 and cols > 1):
+    if (col_stride != 1 and cols > 1) or t.get_device() != device:
         raise ValueError("a matrix of this call is on another device, or its rows are not contiguous")
-    return _PACK_MATRIX(t.data_ptr(), rows, cols, row_stride if rows > 1 else max(cols, 1), _float_type(t.dtype))
+    if rows <= 1:                            # the stride of a single row means nothing
+        row_stride = cols or 1
+    return _PACK_MATRIX(t.data_ptr(), rows, cols, row_stride, (_FLOAT_TYPES or _float_types()).get(t.dtype, -1))
 
 
-def _grouped(q, scale, group: int, columns: int, itemsize: int, device: int):
-    """Check a quantized matrix with a scale per `group` columns: dense tensors of matching shapes on the device."""
-    rows = q.shape[0]
-    if group < 1 or q.dim() != 2 or q.element_size() != 1 or tuple(scale.shape) != (rows, (columns + group - 1) // group) or scale.element_size() != itemsize:
-        raise ValueError("quantized values and scales do not match: one scale per group of columns and row")
+def _grouped(q, scale, group: int, per_byte: int, dtype, device: int):
+    """Check a quantized matrix of `per_byte` values per byte with scales of `dtype` per `group` columns: dense tensors of matching
+    shapes on the device.  Returns its rows and columns."""
+    rows, cols = q.shape
+    cols *= per_byte
+    if group < 1 or scale.shape != (rows, -(-cols // group)) or scale.dtype is not dtype or q.itemsize != 1:
+        raise ValueError("quantized values and scales do not match: bytes, and one scale of the right type per group of columns and row")
     if not (q.is_contiguous() and scale.is_contiguous()) or q.get_device() != device or scale.get_device() != device:
         raise ValueError("quantized values and scales have to be dense and on the handle's device")
-    return rows
+    return rows, cols
 
 
 def to_device(a):
@@ -307,6 +313,9 @@ class Handle:
     def __init__(self, device: int = 0):
         self._h = C.c_void_p()
         self.device = device
+        if not _SAVED_TYPES:
+            import torch
+            _SAVED_TYPES.extend((torch.int8, torch.float32))
         _check(lib().hq_create(device, C.byref(self._h)), "hq_create")
 
     def close(self):
@@ -395,17 +404,14 @@ class Handle:
         return _raw_stream_of(self.device)
 
     def _w4(self, q, scale, group: int, dtype) -> bytes:
-        n = _grouped(q, scale, group, 2 * q.shape[1], 2, self.device)
-        if scale.dtype != dtype:
-            raise ValueError("the scales have to be of the activations' type")
-        return _PACK_W4(q.data_ptr(), scale.data_ptr(), n, 2 * q.shape[1], group)
+        n, k = _grouped(q, scale, group, 2, dtype, self.device)
+        return _PACK_W4(q.data_ptr(), scale.data_ptr(), n, k, group)
 
     def _saved8(self, q, scale, group: int) -> bytes:
-        import torch
-        rows = _grouped(q, scale, group, q.shape[1], 4, self.device)
-        if q.dtype != torch.int8 or scale.dtype != torch.float32:
+        rows, cols = _grouped(q, scale, group, 1, _SAVED_TYPES[1], self.device)
+        if q.dtype is not _SAVED_TYPES[0]:
             raise ValueError("saved activations are int8 with float32 scales")
-        return _PACK_SAVED8(q.data_ptr(), scale.data_ptr(), rows, q.shape[1], group)
+        return _PACK_SAVED8(q.data_ptr(), scale.data_ptr(), rows, cols, group)
 
     def linear_w4(self, x, q, scale, group: int, bias, out):
         """out (m, n) = x (m, k) W^T + bias; q: (n, k / 2) bytes, scale: (n, ceil(k / group)), bias: (n,) or None, all of x's type."""

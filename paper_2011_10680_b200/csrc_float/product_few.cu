@@ -78,6 +78,24 @@ template <class T> __device__ __forceinline__ void to_floats(const uint4& v, flo
   for (int i = 0; i < 8; ++i) f[i] = hq_to_float(t[i]);
 }
 
+// Largest magnitude of eight values, as the bits of a float.  (NaN wins: the 16-bit maxima hand it on.)
+template <class P>
+__device__ __forceinline__ uint32_t largest_pair(const uint4& v) {
+  const uint32_t a = v.x & 0x7fff7fffu, b = v.y & 0x7fff7fffu, c = v.z & 0x7fff7fffu, d = v.w & 0x7fff7fffu;
+  const P m = __hmax2_nan(__hmax2_nan(*(const P*)&a, *(const P*)&b), __hmax2_nan(*(const P*)&c, *(const P*)&d));
+  return *(const uint32_t*)&m;
+}
+template <class T> __device__ __forceinline__ uint32_t largest(const uint4& v);
+template <> __device__ __forceinline__ uint32_t largest<__nv_bfloat16>(const uint4& v) {
+  const uint32_t m = largest_pair<__nv_bfloat162>(v) & 0x7fff7fffu;
+  return max(m << 16, m & 0xffff0000u);
+}
+template <> __device__ __forceinline__ uint32_t largest<__half>(const uint4& v) {
+  const uint32_t m = largest_pair<__half2>(v) & 0x7fff7fffu;       // (as 16-bit integers they are in order too, NaN on top)
+  const __half_raw r{(unsigned short)max(m & 0xffffu, m >> 16)};
+  return __float_as_uint(__half2float(__half(r)));
+}
+
 // Sum of x w over `len` inputs of one output and row, value by value; what lies past k_end is left out.
 template <class T>
 __device__ __noinline__ float by_value_sum(const ProductArgs& p, int i, int row, int from, int len, int k_end) {
@@ -124,6 +142,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
   // the scales of one output, as the aligned words they lie in; those of outputs past the last are never used.
   int f_tile = tile0, f_stage = 0, f_slot = 0;
   const long long all_scales = (long long)p.i * p.groups;
+  long long f_row = (long long)(tile0 * (16 * RT) + lane) * p.groups;       // first scale of this lane's output
+  bool f_live = lane < 16 * RT && tile0 * (16 * RT) + lane < p.i;
   auto fetch = [&]() {
     const uint32_t bar = smem_u32(&ctl.full[warp][f_slot]);
     const int k = k_begin + ((f_stage << a.along_log) + kw) * kStageInputs, row = f_tile * (16 * RT);
@@ -131,11 +151,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
       mbar_expect_tx(bar, kStageBytes);
       tma_load_2d(ring + f_slot * kStageBytes, &map_q, bar, k >> 1, row);
     }
-    if (lane < 16 * RT && row + lane < p.i && k < p.r) {
+    if (f_live && k < p.r) {
       const int first = (int)__umulhi((uint32_t)k >> 4, a.group_mul), last = min(first + 2 * parts - 1, p.groups - 1);
-      const long long at = (long long)(row + lane) * p.groups;
       const uint32_t to = scale_ring + f_slot * kScaleBytes + lane * a.scale_pitch;
-      const long long w0 = (at + first) >> 1, w1 = (at + last) >> 1;
+      const long long w0 = (f_row + first) >> 1, w1 = (f_row + last) >> 1;
 #pragma unroll
       for (int w = 0; w < (WHOLE ? 2 : 5); ++w) {
         if (w0 + w <= w1) {
@@ -146,7 +165,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
     }
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
     if (++f_slot == a.depth) f_slot = 0;
-    if (++f_stage == my_stages) { f_stage = 0; f_tile += tile_stride; }
+    if (++f_stage == my_stages) {
+      f_stage = 0; f_tile += tile_stride;
+      f_row = (long long)(f_tile * (16 * RT) + lane) * p.groups;
+      f_live = lane < 16 * RT && f_tile * (16 * RT) + lane < p.i;
+    }
   };
   const int ahead = min(a.depth, units);
   for (int n = 0; n < ahead; ++n) fetch();
@@ -175,9 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
         if (e - lane + l * kThreads >= all_pieces) break;         // (the whole warp: a row has whole warps of pieces)
         float f[8];
         to_floats<T>(v[l], f);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+        uint32_t top = largest<T>(v[l]);
         beyond = beyond || top >= 0x64000000u;                    // 2^73
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -248,26 +269,35 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
       const uint32_t from = ring + slot * kStageBytes;
       const int st0 = ((stage << a.along_log) + kw) * 2, k0 = k_begin + st0 * kStep;
       if (!kByValue) {
+        // (with one eight of columns both halves of the stage at once: twice the chains of dependent sums)
         float acc[2][RT][NB][4] = {};
+        constexpr int kTogether = NB == 1 ? 2 : 1;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint4 w[2 * RT];
+        for (int half0 = 0; half0 < 2; half0 += kTogether) {
+          uint4 w[kTogether][2 * RT];
 #pragma unroll
-          for (int h = 0; h < 2 * RT; ++h) w[h] = load_shared(from + (row_in_8 + 8 * h) * 128 + (((half * 4 + t) ^ row_in_8) << 4));
+          for (int y = 0; y < kTogether; ++y)
+#pragma unroll
+            for (int h = 0; h < 2 * RT; ++h) w[y][h] = load_shared(from + (row_in_8 + 8 * h) * 128 + ((((half0 + y) * 4 + t) ^ row_in_8) << 4));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint4 b[NB];
+            uint4 b[kTogether][NB];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) b[nb] = load_shared(x_at[nb] + (st0 + half) * x_step[nb] + i * 64);
+            for (int y = 0; y < kTogether; ++y)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-              const uint32_t lo = word(w[2 * r], i), hi = word(w[2 * r + 1], i), lo8 = lo >> 8, hi8 = hi >> 8;
-              const uint32_t a0 = lower(lo, flip), a1 = lower(hi, flip), a2 = upper(lo, flip4), a3 = upper(hi, flip4);
-              const uint32_t c0 = lower(lo8, flip), c1 = lower(hi8, flip), c2 = upper(lo8, flip4), c3 = upper(hi8, flip4);
+              for (int nb = 0; nb < NB; ++nb) b[y][nb] = load_shared(x_at[nb] + (st0 + half0 + y) * x_step[nb] + i * 64);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) {
-                mma(acc[half][r][nb], a0, a1, a2, a3, b[nb].x, b[nb].y);
-                mma(acc[half][r][nb], c0, c1, c2, c3, b[nb].z, b[nb].w);
+            for (int y = 0; y < kTogether; ++y) {
+#pragma unroll
+              for (int r = 0; r < RT; ++r) {
+                const uint32_t lo = word(w[y][2 * r], i), hi = word(w[y][2 * r + 1], i), lo8 = lo >> 8, hi8 = hi >> 8;
+                const uint32_t a0 = lower(lo, flip), a1 = lower(hi, flip), a2 = upper(lo, flip4), a3 = upper(hi, flip4);
+                const uint32_t c0 = lower(lo8, flip), c1 = lower(hi8, flip), c2 = upper(lo8, flip4), c3 = upper(hi8, flip4);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                  mma(acc[half0 + y][r][nb], a0, a1, a2, a3, b[y][nb].x, b[y][nb].y);
+                  mma(acc[half0 + y][r][nb], c0, c1, c2, c3, b[y][nb].z, b[y][nb].w);
+                }
               }
             }
           }
@@ -359,12 +389,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
           }
         };
         for (int e = kw * 32 + lane; e < outputs; e += members) {
+          const int col = ((e / (16 * kHalves)) << parts_log) + (kHalves == 2 ? (e >> 4 & 1) * 8 : 0), turned = (e & 15) ^ ((col >> 1 & 1) << 3);
+          const float* part = sums + col * 16 + turned;            // a row's columns: this one, the next, and two more, turned the other way
+          const int other = 32 + (turned ^ 8) - turned;
           float sum = 0.f;
-          for (int k2 = 0; k2 < along; ++k2) {
-            for (int q = 0; q < parts; ++q) {
-              const int col = ((e / (16 * kHalves)) << parts_log) + q + (kHalves == 2 ? (e >> 4 & 1) * 8 : 0);
-              sum += sums[k2 * kSums + col * 16 + ((e & 15) ^ ((col >> 1 & 1) << 3))];
-            }
+#pragma unroll 4
+          for (int k2 = 0; k2 < along; ++k2, part += kSums) {
+            sum += part[0];
+            if (!WHOLE) sum += part[16];
+            if (!WHOLE && parts == 4) { sum += part[other]; sum += part[other + 16]; }
           }
           if (a.splits == 1) output(e, sum); else ((float*)(shared + a.sum_at))[e] = sum;
         }

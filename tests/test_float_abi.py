@@ -176,12 +176,14 @@ def test_binding_describes_strided_rows_and_refuses_what_it_cannot_describe():
     with pytest.raises(ValueError):
         binding._packed_matrix(FakeTensor((3, 8), (8, 1), torch.float16, device=1), 0)
     q, s = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.float16)
-    for bad_q, bad_s, group in ((q, s, 128), (q, s[:3], 64), (q.t(), s, 64), (q.view(-1), s, 64), (q, s.float(), 64), (q.short(), s, 64), (q, s, 0)):
+    half = torch.float16
+    for bad_q, bad_s, group in ((q, s, 128), (q, s[:3], 64), (q.t(), s, 64), (q.view(-1), s, 64), (q, s.float(), 64), (q.short(), s, 64), (q, s, 0),
+                                (q, torch.zeros(2, 4, dtype=half).t(), 64)):
         with pytest.raises(ValueError):
-            binding._grouped(bad_q, bad_s, group, 128, 2, -1)
-    assert binding._grouped(q, s, 64, 128, 2, -1) == 4
+            binding._grouped(bad_q, bad_s, group, 2, half, -1)
+    assert binding._grouped(q, s, 64, 2, half, -1) == (4, 128)
     with pytest.raises(ValueError):
-        binding._grouped(q, s, 64, 128, 2, 0)                                                           # host memory
+        binding._grouped(q, s, 64, 2, half, 0)                                                          # host memory
 
 
 @pytest.mark.parametrize("scale_type", ["bf16", "fp16"])
