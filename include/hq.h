@@ -332,7 +332,10 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
  *     neither of them above 2^30 (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;
  *   - no call allocates or needs scratch memory: calls through one handle may run on several streams at once,
  *     and can be captured into graphs;
- *   - infinities and NaN go through the arithmetic as IEEE has them.
+ *   - products run on the tensor cores where rows start on 16 bytes: strides of 16-bit matrices a multiple of 8 (any
+ *     number of columns), k of hq_w4 a multiple of 32, cols of a saved matrix a multiple of 16; other shapes take a
+ *     plain and much slower kernel with the same results up to rounding;
+ *   - infinities and NaN go through the arithmetic as IEEE has them; an expired device-side wait is reported by hq_sync.
  * ===================================================================================================== */
 typedef enum { HQ_F32 = 0, HQ_F16 = 1, HQ_BF16 = 2 } hq_float_type;
 
@@ -367,8 +370,8 @@ typedef enum {
 /*
  * Linear layer:  out[m][i] = bias[i] + sum_j x[m][j] * w[i][j].
  * x: (m, k), out: (m, n), both HQ_F16 or HQ_BF16 and of one type; bias: n values of that type or NULL.  With few rows (one token
- * of each of a few sequences: up to 16, or 8 / 4 where two / four groups share 128 inputs) the weights' integers enter the
- * products and a group's sum is scaled in 32 bits; with more, each w[i][j] is first rounded to the type of x, as a 16-bit
+ * of each of a few sequences: up to 16, or 8 / 4 where two / four groups share 128 inputs, as long as they fit in shared
+ * memory) the weights' integers enter the products and a group's sum is scaled in 32 bits; with more, each w[i][j] is first rounded to the type of x, as a 16-bit
  * weight matrix would hold it.
  */
 hq_status hq_linear_w4(hq_handle* h, const hq_matrix* x, const hq_w4* w, const void* bias, hq_matrix* out, void* stream);

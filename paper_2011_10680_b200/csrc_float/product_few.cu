@@ -476,7 +476,7 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
   bool found = false;
   for (int splits = 1; splits <= 8; splits *= 2) {
     const int per = (all + splits - 1) / splits, clusters = sm_count / splits;
-    if (splits > 1 && (splits - 1) * per >= all) break;                // a CTA without inputs
+    if (clusters < 1 || (splits > 1 && (splits - 1) * per >= all)) break;     // a CTA without inputs
     const long long inputs = (long long)per * kStageInputs;
     const long long pitch = inputs * 2 + 64;                           // 64 modulo 128: eight lanes' pieces lie on different banks
     const long long x_bytes = (256 + p.j * pitch + 1023) & ~1023ll, fix_bytes = (inputs / kStep * 8 * nb * 8 + 127) & ~127ll;

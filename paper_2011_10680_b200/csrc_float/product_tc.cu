@@ -4,10 +4,15 @@
 // NT <= 256 columns.  Both come by TMA as they are stored, A into a ring of its own, from which warps restore each value in the type
 // of B - (integer - offset) * scale, one rounding - and write the swizzled tile the MMA reads.  FORWARD tiles are K-major; DGRAD and
 // WGRAD reduce over the rows of what is stored, their tiles are MN-major, so no operand is ever transposed by hand.
-// Roles: one thread fetches, one issues MMAs, four groups of four warps convert A, each every fourth stage (a stage takes a warp
-// longer than its MMAs take), four warps drain the accumulators; CTAs are persistent and have two accumulators, so that a tile is
-// drained while the next one is computed.  When there are too few tiles to go round, the CTAs of a cluster share a tile's
+// Roles: one thread fetches, one issues MMAs, groups of warps convert A, taking the stages in turn, four warps drain the accumulators;
+// CTAs are persistent and have two accumulators, so that a tile is drained while the next one is computed.  With many columns two
+// CTAs share their MMAs (cta_group::2).  When there are too few tiles to go round, the CTAs or pairs of a cluster share a tile's
 // reduction and add their parts in rank order through distributed shared memory.
+//
+// What bounds it.  256 columns: the tensor cores under the power cap - 4001 tokens, 16384 x 4096 bf16 in 391 us alone (1373 TFLOP/s, 0.82
+// of the measured burst, at the sustained rate), 459 us back to back; 8192 x 16384 x 4096 fp16 gradient 776 us (1416).  Few
+// columns: the converters' instructions, 17 per eight 4-bit weights and about 600 cycles a stage, and some 4 us before the first
+// MMA and behind the last - 48 tokens, 8192 x 8192: 29 us, 1.3 TB/s.
 #include "../csrc/tc_common.cuh"
 #include "float_internal.cuh"
 
@@ -18,16 +23,21 @@ constexpr int kStep = 64;                         // values of the reduction per
 constexpr int kTileABytes = kTileC * kStep * 2;
 
 // Roles by warp.  A warp's scheduler is its number modulo four, and the threads that fetch and issue MMAs, which every stage waits
-// for, share theirs with no converter: beside four of them each of their few instructions took 14 cycles (48 tokens, 8192 x 8192:
-// SCHED_BEFORE us, so SCHED_AFTER).  Accumulator lanes 32 q .. 32 q + 31 belong to warps 4 n + q.
+// for, share theirs with few converters or none: beside four of them each of their instructions takes some 14 cycles (48 tokens,
+// 8192 x 8192, with groups of four warps: 34.3 us, apart 33.5).  Accumulator lanes 32 q .. 32 q + 31 belong to warps 4 n + q.
 enum Role { ROLE_FETCH, ROLE_MMA, ROLE_ALLOC, ROLE_CONVERT, ROLE_DRAIN };
 __device__ __forceinline__ Role role_of(int warp) {
   if (warp & 3) return warp < 24 ? ROLE_CONVERT : ROLE_DRAIN;
   return warp == 0 ? ROLE_FETCH : warp == 4 ? ROLE_MMA : warp == 8 ? ROLE_ALLOC : warp == 12 ? ROLE_DRAIN : ROLE_CONVERT;
 }
-// Converter warps by number: first the eighteen on schedulers of their own, then the three beside the issuers.
+// Converter warps by number: eighteen on schedulers of their own, and three beside the issuers, which come last (`beside_first`: first;
+// with few columns a stage is bound by the converters' instructions, and a fourth scheduler helps more than it hinders: 48 tokens,
+// 8192 x 8192: 30.5 us, so 29.0; 4001 tokens, 16384 x 4096, on pairs: 389 us, so 394).
 constexpr int kMaxConverters = 21;
-__device__ __forceinline__ int converter_number(int warp) { return warp & 3 ? (warp >> 2) * 3 + (warp & 3) - 1 : 18 + (warp >> 2) - 4; }
+__device__ __forceinline__ int converter_number(int warp, bool beside_first) {
+  if (warp & 3) return (beside_first ? 3 : 0) + (warp >> 2) * 3 + (warp & 3) - 1;
+  return (beside_first ? 0 : 18) + (warp >> 2) - 4;
+}
 
 // One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages; DGRAD 64 rows of 64 bytes and WGRAD 64
 // rows of 128 bytes, one stage.
@@ -397,8 +407,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         drain_wait(smem_u32(&ctl.drain), 0, a.status);
       }
     }
-  } else if (role == ROLE_CONVERT && converter_number(warp) < kGroups * kConverterWarps) {
-    const int number = converter_number(warp);
+  } else if (role == ROLE_CONVERT && converter_number(warp, !kPair || KIND == PRODUCT_WGRAD) < kGroups * kConverterWarps) {
+    const int number = converter_number(warp, !kPair || KIND == PRODUCT_WGRAD);
     const int group = number / kConverterWarps, member = number % kConverterWarps;
     // (two warps: the halves of the lanes, or 64 rows each; four: halves and 32 rows, or 32 rows)
     const int row0 = (KIND == PRODUCT_FORWARD ? member * 32 * kRowsPerThread : kRowsPerThread == 2 ? 0 : (member & 1) * 32) + lane;
@@ -581,17 +591,19 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
   a.status = h->dev_status;
   a.steps = (p.r + kStep - 1) / kStep;
   // Columns per tile and CTAs (or pairs) per tile: what is through first, by the cycles that a stage, a tile and the joining of parts
-  // took (stages of 32 / 64 / 128 / 256 columns: STAGE_CYCLES).
+  // take (a stage, counted in the kernel: 650 with 256 columns on a pair, about 600 with 64, 32 and with saved activations).
   int nt = 0;
   long long best = 0;
   for (const int width : {32, 64, 128, 256}) {
-    const int ctas = width == 256 ? 2 : 1, stage = width == 256 ? 620 : width == 128 ? 560 : width == 64 ? 450 : 430;
+    const int ctas = width == 256 ? 2 : 1, stage = width == 256 ? 650 : width == 128 ? 620 : 600;
     const long long i_tiles = (p.i + ctas * kTileC - 1) / (ctas * kTileC), tiles = i_tiles * ((p.j + width - 1) / width);
     if (tiles > 0x3fffffff) continue;
     for (int splits = 1; splits * ctas <= 8; splits *= 2) {
       const int split_steps = (a.steps + splits - 1) / splits;
       if (splits > 1 && ((splits - 1) * split_steps >= a.steps || split_steps < 4)) break;
-      const long long at_once = h->sm_count / (ctas * splits), rounds = (tiles + at_once - 1) / at_once;
+      const long long at_once = h->sm_count / (ctas * splits);
+      if (at_once < 1) break;
+      const long long rounds = (tiles + at_once - 1) / at_once;
       if (splits > 1 && rounds > 1) break;
       const long long cost = rounds * ((long long)split_steps * stage + 1500) + (splits > 1 ? 3000 + 10 * width : 0);
       if (best && cost >= best) continue;

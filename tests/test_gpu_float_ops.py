@@ -109,6 +109,8 @@ LINEAR = [
     (1, 1, 32, 32), (1, 16, 128, 128), (1, 17, 128, 64), (1, 100, 96, 32), (2, 33, 160, 64), (3, 64, 256, 96), (7, 129, 512, 128),
     (8, 48, 2048, 256), (9, 31, 640, 32), (15, 257, 384, 64), (16, 128, 1024, 4096), (1, 1000, 2048, 128), (5, 40, 4096, 128),
     (1, 2300, 416, 32), (4, 4113, 128, 128), (16, 16, 8192, 64),
+    # few outputs and many inputs, or rows too long for one CTA: the CTAs of a cluster share the inputs
+    (1, 64, 16384, 128), (2, 40, 32768, 64), (16, 48, 16384, 128), (4, 33, 12288, 32), (3, 2500, 16416, 128), (9, 700, 8224, 8224),
     (17, 128, 64, 32), (18, 1, 32, 32), (31, 130, 96, 64), (32, 64, 128, 128), (33, 129, 160, 32), (48, 300, 512, 256), (64, 128, 1024, 64),
     (65, 127, 192, 96), (100, 200, 288, 128), (129, 257, 320, 64), (256, 128, 256, 128), (257, 384, 448, 32), (300, 513, 1056, 128),
     (1000, 640, 128, 32), (513, 1030, 2080, 96), (2, 3000, 32, 64), (700, 96, 4096, 128),
@@ -178,6 +180,40 @@ def test_linear_w4_results_beyond_fp16_are_infinite(hq):
         assert hq.linear_w4(x, q, s, 128, None, out) == 0
         hq.sync()
         assert bool(torch.isinf(out).all())                    # 128 * 100 * 56 = 716800
+
+
+def test_linear_w4_rows_that_do_not_fit_on_chip(hq):
+    """Few rows, but longer than the shared memory of a cluster: the path of many rows takes them, with its rounding."""
+    m, n, k, group = 16, 72, 131072, 128
+    g = gen(6)
+    q, s, w = random_w4(g, n, k, group, BF16)
+    x = normal(g, m, k).to(BF16)
+    out = out_matrix(m, n, BF16)
+    assert hq.linear_w4(x, q, s, group, None, out) == 0
+    hq.sync()
+    check_product(out, x.double() @ w.t(), x.double().abs() @ w.abs().t(), k, BF16, True)
+
+
+@pytest.mark.parametrize("exponent", [-126, -100, -30, 50, 80, 100])
+@pytest.mark.parametrize("m", [1, 8, 40])
+def test_linear_w4_magnitudes(hq, m, exponent):
+    """Activations across the range of bfloat16, rows of different magnitude beside one another, one element far above its row."""
+    g = gen(7)
+    n, k, group = 96, 512, 64
+    q, s, w = random_w4(g, n, k, group, BF16)
+    x = normal(g, m, k) * 2.0 ** exponent
+    x[0] *= 2.0 ** 12
+    x[m - 1, 7] *= 2.0 ** 14
+    x = x.to(BF16)
+    out = out_matrix(m, n, BF16)
+    assert hq.linear_w4(x, q, s, group, None, out) == 0
+    hq.sync()
+    ref, magnitude = x.double() @ w.t(), x.double().abs() @ w.abs().t()
+    # (besides the usual: values far below the largest of their 128 inputs are held to 2^-36 of it, integers up to 15 and as many terms)
+    beyond = x.double().abs().amax(dim=1, keepdim=True) * 2.0 ** -36 * 16 * k * float(s.double().max())
+    err = (out.double() - ref).abs()
+    bound = u(BF16) * ref.abs() * 1.01 + magnitude * (u(BF16) * rounds_weights(m, k, group) + (k + 16) * 2.0 ** -24) + beyond + 2.0 ** -133
+    assert bool((err <= bound).all()), float((err / bound).max())
 
 
 @pytest.mark.parametrize("m", [1, 40])
