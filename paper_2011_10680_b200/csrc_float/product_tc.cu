@@ -13,6 +13,8 @@
 // of the measured burst, at the sustained rate), 459 us back to back; 8192 x 16384 x 4096 fp16 gradient 776 us (1416).  Few
 // columns: the converters' instructions, 17 per eight 4-bit weights and about 600 cycles a stage, and some 4 us before the first
 // MMA and behind the last - 48 tokens, 8192 x 8192: 29 us, 1.3 TB/s.
+#include <type_traits>
+
 #include "../csrc/tc_common.cuh"
 #include "float_internal.cuh"
 
@@ -63,7 +65,7 @@ struct Shape {
   static constexpr int kUnits = kRawBytes / Unit<KIND>::kBytes;
   static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
   static constexpr int kRowsPerThread = kWgrad ? 1 : 2, kConverterWarps = 4 / kRowsPerThread;
-  static constexpr int kGroups = kWgrad ? 5 : kStages;
+  static constexpr int kGroups = kWgrad ? 4 : kStages;             // (saved activations: five were no faster)
   static_assert(kGroups <= kStages && kGroups <= Unit<KIND>::kStagesOf * kUnits && kGroups * kConverterWarps <= kMaxConverters && kUnits <= 8 && kStages <= 8);
 };
 
@@ -190,50 +192,57 @@ __device__ __forceinline__ void convert8(uint32_t w, unsigned long long scale2, 
   hi = out[1];
 }
 
-// The scales of a converter thread's rows of a stage, one per half of a row's 64 integers, fetched a turn of its group ahead.
+// The scales of a converter thread's rows of a stage, one per half of a row's 64 integers, fetched a turn of its group ahead.  Within a
+// tile the thread's rows (not FORWARD) move on by a fixed step.
 template <int KIND, class T, int ROWS>
 struct Scales {
+  using S = typename std::conditional<KIND == PRODUCT_WGRAD, float, T>::type;
   const ProductArgs& p;
+  const uint32_t group_mul;
   const int row_part, lane_part;   // first of the rows (the second is 32 further on), and the first lane of the half (not FORWARD)
-  const uint8_t* base;
-  bool exists[2];                  // FORWARD: the row; else the half's columns
+  const S* at;                     // FORWARD: of the first row; else the first scale of the stage to be loaded
+  int along;                       // FORWARD: first input of the stage to be loaded; else its first row
+  bool exists[2];                  // FORWARD: the rows; else the halves' columns
   int second;                      // from the first half's scale to the second's (not FORWARD)
+  long long step;                  // from one turn of the group to the next (not FORWARD)
 
-  __device__ __forceinline__ Scales(const ProductArgs& args, int row, int half) : p(args), row_part(row), lane_part(half * 64) {}
-  __device__ __forceinline__ void enter(int i0, bool tile_exists) {
+  __device__ __forceinline__ Scales(const ProductArgs& args, uint32_t mul, int row, int half, int groups)
+      : p(args), group_mul(mul), row_part(row), lane_part(half * 64), step((long long)groups * kStep * args.groups) {}
+  // stage `st` of the reduction, in the tile of lanes from i0
+  __device__ __forceinline__ void enter(int i0, bool tile_exists, int st) {
     if (KIND == PRODUCT_FORWARD) {
       const long long row = i0 + row_part;
       exists[0] = tile_exists && row < p.i;
       exists[1] = tile_exists && row + 32 < p.i;
-      base = (const uint8_t*)p.scale + row * p.groups * sizeof(T);
+      at = (const S*)p.scale + row * p.groups;
+      along = st * kStep;
     } else {
-      const int col = i0 + lane_part;
+      const int col = i0 + lane_part, g = col / p.group;
       exists[0] = tile_exists && col < p.i;
       exists[1] = tile_exists && col + 32 < p.i;
-      second = (col + 32) / p.group - col / p.group;
-      base = (const uint8_t*)p.scale + (long long)(col / p.group) * (KIND == PRODUCT_DGRAD ? sizeof(T) : sizeof(float));
+      second = (col + 32) / p.group - g;
+      along = st * kStep + row_part;
+      at = (const S*)p.scale + (long long)along * p.groups + g;
     }
   }
-  // of stage `st` of the tile entered, [row][half]; zero for what does not exist
-  __device__ __forceinline__ void load(int st, uint32_t group_mul, float (&scale)[ROWS][2]) const {
+  // zero for what does not exist; then `turns` stages on
+  __device__ __forceinline__ void load(int turns, float (&scale)[ROWS][2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int k = st * kStep + 32 * h;
+      const int k = along + 32 * h;
       const uint32_t g = KIND != PRODUCT_FORWARD ? 0 : group_mul ? __umulhi((uint32_t)k >> 4, group_mul) : (uint32_t)k / (uint32_t)p.group;
 #pragma unroll
       for (int x = 0; x < ROWS; ++x) {
         scale[x][h] = 0.f;
         if (KIND == PRODUCT_FORWARD) {
-          if (exists[x] && k < p.r) scale[x][h] = hq_to_float(((const T*)base)[(long long)x * 32 * p.groups + g]);
-        } else {
-          const long long row = st * kStep + row_part + 32 * x;
-          if (exists[h] && row < p.r) {
-            if (KIND == PRODUCT_DGRAD) scale[x][h] = hq_to_float(((const T*)base)[row * p.groups + h * second]);
-            else scale[x][h] = ((const float*)base)[row * p.groups + h * second];
-          }
+          if (exists[x] && k < p.r) scale[x][h] = hq_to_float(at[(x ? 32ll * p.groups : 0ll) + g]);
+        } else if (exists[h] && along + 32 * x < p.r) {
+          scale[x][h] = hq_to_float(at[(x ? 32ll * p.groups : 0ll) + (h ? second : 0)]);
         }
       }
     }
+    along += turns * kStep;
+    if (KIND != PRODUCT_FORWARD) at += step;
   }
 };
 
@@ -407,8 +416,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
         drain_wait(smem_u32(&ctl.drain), 0, a.status);
       }
     }
-  } else if (role == ROLE_CONVERT && converter_number(warp, !kPair || KIND == PRODUCT_WGRAD) < kGroups * kConverterWarps) {
-    const int number = converter_number(warp, !kPair || KIND == PRODUCT_WGRAD);
+  } else if (role == ROLE_CONVERT && converter_number(warp, !kPair) < kGroups * kConverterWarps) {
+    const int number = converter_number(warp, !kPair);
     const int group = number / kConverterWarps, member = number % kConverterWarps;
     // (two warps: the halves of the lanes, or 64 rows each; four: halves and 32 rows, or 32 rows)
     const int row0 = (KIND == PRODUCT_FORWARD ? member * 32 * kRowsPerThread : kRowsPerThread == 2 ? 0 : (member & 1) * 32) + lane;
@@ -423,11 +432,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       while (st >= padded && tile < a.tiles) { st -= padded; tile += stride; before += steps; before_padded += padded; moved = true; }
       return moved;
     };
-    Scales<KIND, T, kRowsPerThread> scales(p, row0, half);
+    Scales<KIND, T, kRowsPerThread> scales(p, a.group_mul, row0, half, kGroups);
     settle();
-    scales.enter(i_of(tile), tile < a.tiles);
+    scales.enter(i_of(tile), tile < a.tiles, begin + st);
     float scale[kRowsPerThread][2];
-    scales.load(begin + st, a.group_mul, scale);
+    scales.load(kGroups, scale);
     while (tile < a.tiles) {
       const unsigned n = before + st, v = before_padded + st, unit_no = v / kPer;
       const bool real = st < steps;
@@ -450,8 +459,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       }
       if (lane == 0) mbar_arrive(smem_u32(&ctl.raw_empty[u]));
       st += kGroups;
-      if (settle()) scales.enter(i_of(tile), tile < a.tiles);
-      scales.load(begin + st, a.group_mul, scale);               // (behind the fence, which waits for loads too)
+      if (settle()) scales.enter(i_of(tile), tile < a.tiles, begin + st);
+      scales.load(kGroups, scale);                               // (behind the fence, which waits for loads too)
     }
   } else if (role == ROLE_DRAIN) {
     const int quad = warp & 3;
