@@ -48,17 +48,28 @@ hq_status check_saved(const hq_saved8* s, long long rows, long long cols) {
   return aligned(s->q, 16) && aligned(s->scale, 16) ? HQ_OK : HQ_ERR_ALIGNMENT;
 }
 
+// A launch that failed leaves no error behind for the caller's next CUDA call.
+inline hq_status launched(cudaError_t e) {
+  if (e == cudaSuccess) return HQ_OK;
+  cudaGetLastError();
+  return HQ_ERR_CUDA;
+}
+inline hq_status launched(hq_status st) {
+  if (st == HQ_ERR_CUDA) cudaGetLastError();
+  return st;
+}
+
 inline int groups_of(long long cols, int group) { return (int)((cols + group - 1) / group); }
 
 hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
-  if (kind == PRODUCT_FORWARD && hq_product_few_supported(a)) return hq_launch_product_few(h, type, a, (cudaStream_t)stream);
+  if (kind == PRODUCT_FORWARD && hq_product_few_supported(a)) return launched(hq_launch_product_few(h, type, a, (cudaStream_t)stream));
   if (hq_product_tc_supported(kind, a)) {
-    const hq_status st = hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream);
+    const hq_status st = launched(hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream));
     if (st != HQ_ERR_UNSUPPORTED) return st;
   }
-  return hq_launch_product_any(kind, type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+  return launched(hq_launch_product_any(kind, type, a, (cudaStream_t)stream));
 }
 
 // What hq_act_save8 and hq_act_backward8 share.
@@ -143,7 +154,7 @@ hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, 
   if (y) { a.y = y->data; a.y_stride = y->row_stride; }
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
-  return hq_launch_act_save8(x->type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+  return launched(hq_launch_act_save8(x->type, a, (cudaStream_t)stream));
 }
 
 hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act,
@@ -161,7 +172,7 @@ hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
   if (dgate) { a.dgate = dgate->data; a.dgate_stride = dgate->row_stride; }
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
-  return hq_launch_act_backward8(dy->type, a, (cudaStream_t)stream) == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
+  return launched(hq_launch_act_backward8(dy->type, a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -2,6 +2,8 @@
 // in 8 bits).  They live apart from csrc/, the integer-only inference pipeline, which holds no floating point.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -59,5 +61,15 @@ hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& a, cu
 bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a);
 hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
 cudaError_t hq_launch_product_any(ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
+// Runs `set` the first time for the current device (its kernels' attributes stay set); again after a failure.
+template <class Set>
+inline bool hq_once_per_device(std::atomic<bool> (&done)[64], Set set) {
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  if (device < 64 && done[device].load()) return true;
+  if (!set()) return false;
+  if (device < 64) done[device].store(true);
+  return true;
+}
 cudaError_t hq_launch_act_save8(int type, const ActArgs& a, cudaStream_t s);
 cudaError_t hq_launch_act_backward8(int type, const ActArgs& a, cudaStream_t s);

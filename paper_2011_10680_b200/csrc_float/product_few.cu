@@ -522,7 +522,10 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
 
 }  // namespace
 
-bool hq_product_few_init() { return load_driver_entry_points() && allow_type<__half>() && allow_type<__nv_bfloat16>(); }
+bool hq_product_few_init() {
+  static std::atomic<bool> done[64];
+  return load_driver_entry_points() && hq_once_per_device(done, [] { return allow_type<__half>() && allow_type<__nv_bfloat16>(); });
+}
 
 bool hq_product_few_supported(const ProductArgs& p) {
   if (p.j > kMaxColumns || p.j * parts_of(p) > kMaxColumns || p.q_cols % 32 || (p.b_stride % 8 && p.j > 1)) return false;

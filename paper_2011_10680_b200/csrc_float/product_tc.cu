@@ -584,8 +584,11 @@ bool allow_kinds() { return allow_widths<PRODUCT_FORWARD, T>() && allow_widths<P
 
 }  // namespace
 
-// Once per device, from hq_create.
-bool hq_product_tc_init() { return load_driver_entry_points() && allow_kinds<__half>() && allow_kinds<__nv_bfloat16>(); }
+// From hq_create.
+bool hq_product_tc_init() {
+  static std::atomic<bool> done[64];
+  return load_driver_entry_points() && hq_once_per_device(done, [] { return allow_kinds<__half>() && allow_kinds<__nv_bfloat16>(); });
+}
 
 bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a) {
   if (a.r < 1) return false;
