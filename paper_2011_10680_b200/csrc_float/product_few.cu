@@ -171,8 +171,6 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
       f_live = lane < 16 * RT && f_tile * (16 * RT) + lane < p.i;
     }
   };
-  const int ahead = min(a.depth, units);
-  for (int n = 0; n < ahead; ++n) fetch();
 
   // x, zeros behind its end up to whole stages, and a step of zeros in front, which the columns without inputs read.
   const int pieces = stages * (kStageInputs / 8), all_pieces = pieces * p.j;
@@ -181,9 +179,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
   {
     constexpr int kLoads = 4;                                     // in flight per thread
     int row = 0, c = threadIdx.x;
-    for (int e = threadIdx.x; e - lane < all_pieces; e += kLoads * kThreads) {
-      uint4 v[kLoads];
-      int row_of[kLoads], c_of[kLoads];
+    uint4 v[kLoads];
+    int row_of[kLoads], c_of[kLoads];
+    auto load_x = [&]() {
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
         while (c >= pieces && row < p.j) { c -= pieces; ++row; }
@@ -193,6 +191,12 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
         if (row < p.j && k < k_end) v[l] = *(const uint4*)((const T*)p.b + row * p.b_stride + k);
         c += kThreads;
       }
+    };
+    load_x();                                                     // (first of all: what everything else waits for)
+    const int ahead = min(a.depth, units);
+    for (int n = 0; n < ahead; ++n) fetch();
+    for (int e = threadIdx.x; e - lane < all_pieces; e += kLoads * kThreads) {
+      if (e != threadIdx.x) load_x();
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
         if (e - lane + l * kThreads >= all_pieces) break;         // (the whole warp: a row has whole warps of pieces)
