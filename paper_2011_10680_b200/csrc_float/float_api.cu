@@ -5,11 +5,14 @@ namespace {
 
 constexpr long long kMaxExtent = 1ll << 30;     // 32-bit indexes of a tile or a group may reach past the last row or column
 
-// The handle's device for the duration of a call.
+// The handle's device for the duration of a call.  A host thread that has made no call to the runtime yet has no context, which
+// encoding a tensor map needs; cudaSetDevice gives it one.
 class DeviceScope {
  public:
   explicit DeviceScope(int device) {
-    ok_ = cudaGetDevice(&before_) == cudaSuccess && (before_ == device || cudaSetDevice(device) == cudaSuccess);
+    thread_local bool has_context = false;
+    ok_ = cudaGetDevice(&before_) == cudaSuccess && ((before_ == device && has_context) || cudaSetDevice(device) == cudaSuccess);
+    has_context = has_context || ok_;
     changed_ = ok_ && before_ != device;
   }
   ~DeviceScope() { if (changed_) cudaSetDevice(before_); }
@@ -64,7 +67,7 @@ inline int groups_of(long long cols, int group) { return (int)((cols + group - 1
 hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
   const DeviceScope device(h->device);
   if (!device.ok()) return HQ_ERR_CUDA;
-  if (kind == PRODUCT_FORWARD && hq_product_few_supported(a)) return launched(hq_launch_product_few(h, type, a, (cudaStream_t)stream));
+  if (kind == PRODUCT_FORWARD && hq_product_few_supported(a, h->sm_count)) return launched(hq_launch_product_few(h, type, a, (cudaStream_t)stream));
   if (hq_product_tc_supported(kind, a)) {
     const hq_status st = launched(hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream));
     if (st != HQ_ERR_UNSUPPORTED) return st;

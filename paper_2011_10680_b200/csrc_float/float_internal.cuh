@@ -55,7 +55,7 @@ __device__ __forceinline__ int hq_nibble(const uint8_t* row, int col) {
 }
 
 // Up to 16 rows of FORWARD (product_few.cu).
-bool hq_product_few_supported(const ProductArgs& a);
+bool hq_product_few_supported(const ProductArgs& a, int sm_count);
 hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& a, cudaStream_t s);
 // On the tensor cores (product_tc.cu): every shape whose rows start on 16 bytes.  hq_launch_product_any takes all of them.
 bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a);

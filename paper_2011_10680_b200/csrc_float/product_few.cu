@@ -531,11 +531,11 @@ bool hq_product_few_init() {
   return load_driver_entry_points() && hq_once_per_device(done, [] { return allow_type<__half>() && allow_type<__nv_bfloat16>(); });
 }
 
-bool hq_product_few_supported(const ProductArgs& p) {
+bool hq_product_few_supported(const ProductArgs& p, int sm_count) {
   if (p.j > kMaxColumns || p.j * parts_of(p) > kMaxColumns || p.q_cols % 32 || (p.b_stride % 8 && p.j > 1)) return false;
   FewArgs a{};
   int rt, shared;
-  return plan(p, 148, a, rt, shared);
+  return plan(p, sm_count, a, rt, shared);
 }
 
 hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& p, cudaStream_t s) {

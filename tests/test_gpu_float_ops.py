@@ -640,6 +640,72 @@ def test_block_is_reproducible_captured_and_on_another_stream(hq):
         hq2.close()
 
 
+def test_block_from_several_host_threads(hq):
+    """One handle, four threads with a stream each: calls overlap on the host and on the GPU, and every result keeps its bits."""
+    import threading
+    want = block_state(70, 702)
+    block(hq, want)
+    hq.sync()
+    states = [block_state(70, 702) for _ in range(4)]
+    torch.cuda.synchronize()
+    done = []
+
+    def worker(t):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                block(hq, t)
+        stream.synchronize()
+        done.append(t)
+    threads = [threading.Thread(target=worker, args=(t,)) for t in states]
+    for thread in threads:
+        thread.start()
+    for thread in threads:
+        thread.join()
+    hq.sync()
+    assert len(done) == 4
+    for t in states:
+        assert all(torch.equal(t[k].view(torch.uint8), want[k].view(torch.uint8)) for k in RESULTS)
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    """No call has to run once before a capture: a new process whose first call of every operator and kernel is captured."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    program = """
+import torch
+import test_gpu_float_ops as ops
+from paper_2011_10680_b200 import binding
+hq = binding.Handle(0)
+t = ops.block_state(70, 702)
+odd_q, odd_s, _ = ops.random_w4(ops.gen(1), 96, 70, 32, ops.BF16)
+odd_x, odd_out = ops.normal(ops.gen(2), 9, 70).to(ops.BF16), ops.out_matrix(9, 96, ops.BF16)
+few_x, few_out = t["x"][:3], ops.out_matrix(3, 640, ops.BF16)
+graph = torch.cuda.CUDAGraph()
+def calls():
+    ops.block(hq, t)
+    assert hq.linear_w4(odd_x, odd_q, odd_s, 32, None, odd_out) == 0
+    assert hq.linear_w4(few_x, *t["w_up"], 64, None, few_out) == 0
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+results = [t[k] for k in ops.RESULTS] + [odd_out, few_out]
+captured = [r.clone() for r in results]
+for r in results:
+    r.zero_()
+calls()
+hq.sync()
+assert all(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)) for a, b in zip(captured, results))
+print("same")
+"""
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([os.path.dirname(here), here, os.environ.get("PYTHONPATH", "")]))
+    run = subprocess.run([sys.executable, "-c", program], env=env, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "same" in run.stdout, run.stderr[-2000:]
+
+
 def test_quantized_by_the_offline_tool(hq):
     """A float matrix through the offline quantizer: the layer's result is that of the quantized weights, near the float one."""
     import numpy as np
