@@ -404,6 +404,23 @@ hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
  */
 hq_status hq_linear_wgrad8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved, hq_matrix* dw, void* stream);
 
+/* Debug aid: the kernel and the launch that a product of these sizes takes on a GPU with `sm_count` SMs, all rows dense.  Host
+ * arithmetic: no GPU is needed.  (`m` tokens, a layer of `n` outputs and `k` inputs, `group` as in the call.) */
+typedef enum { HQ_PRODUCT_LINEAR = 0, HQ_PRODUCT_DGRAD = 1, HQ_PRODUCT_WGRAD = 2 } hq_product;
+typedef enum { HQ_KERNEL_CUDA_CORES = 0, HQ_KERNEL_FEW_ROWS = 1, HQ_KERNEL_TENSOR_MEMORY = 2 } hq_product_kernel;
+typedef struct {              /* all but `kernel` are 0 on the CUDA cores */
+  int32_t kernel;             /* hq_product_kernel */
+  int32_t columns;            /* of a tile (tensor memory; 256: on pairs of CTAs) or of the matrix instructions (few rows) */
+  int32_t outputs;            /* the tile's other side */
+  int32_t splits;             /* CTAs, or pairs of them, that share the reduction of a tile */
+  int32_t steps;              /* stages of each, per tile */
+  int32_t rounds;             /* tiles that the busiest CTA, pair or team of warps computes */
+  int32_t stages;             /* of the operand ring (tensor memory) or of a warp's ring (few rows) */
+  int32_t groups;             /* of converter warps, which take the stages in turn; few rows: warps of a team */
+  int32_t units, unit_stages; /* tensor memory: places of the quantized operand's ring, and the stages that one holds */
+} hq_product_plan;
+hq_status hq_linear_plan(int32_t product, int32_t m, int32_t n, int32_t k, int32_t group, int32_t sm_count, hq_product_plan* plan);
+
 const char* hq_status_string(hq_status s);
 
 #ifdef __cplusplus

@@ -25,7 +25,7 @@ EXPORTS = [
     "hq_network_destroy", "hq_set_conv_path", "hq_set_tile_order", "hq_status_string", "hq_network_time_layers", "hq_conv2d_noalloc", "hq_expire_wait_selftest",
     "hq_network_check_guards", "hq_conv2d_noalloc_sync", "hq_mma_peak_launch",
     "hq_ilp_solve", "hq_concat_requant", "hq_sumpool", "hq_conv2d_plan",
-    "hq_linear_w4", "hq_linear_w4_dgrad", "hq_act_save8", "hq_act_backward8", "hq_linear_wgrad8",
+    "hq_linear_w4", "hq_linear_w4_dgrad", "hq_act_save8", "hq_act_backward8", "hq_linear_wgrad8", "hq_linear_plan",
 ]
 HQ_ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
@@ -80,6 +80,10 @@ class hq_saved8(C.Structure):
     _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("group", C.c_int32)]
 
 
+class hq_product_plan(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("kernel", "columns", "outputs", "splits", "steps", "rounds", "stages", "groups", "units", "unit_stages")]
+
+
 _lib = None
 
 
@@ -126,6 +130,7 @@ def lib():
         L.hq_act_save8.argtypes = [vp, st, st, i32, st, st, st, vp]
         L.hq_act_backward8.argtypes = [vp, st, st, st, i32, st, st, vp]
         L.hq_linear_wgrad8.argtypes = [vp, st, st, st, vp]
+        L.hq_linear_plan.argtypes = [i32] * 6 + [C.POINTER(hq_product_plan)]
         L.hq_status_string.argtypes = [i32]
         L.hq_status_string.restype = C.c_char_p
         for name in EXPORTS:
@@ -477,6 +482,17 @@ def conv2d_plan(n, h, w, cin, cout, k, stride, pad, out_bits=8, residual_bits=0,
         return None
     _check(st, "hq_conv2d_plan")
     return {**{name: getattr(plan, name) for name, _ in hq_conv_plan._fields_}, "shape": HQ_SHAPE[plan.shape]}
+
+
+HQ_PRODUCT = {"linear": 0, "dgrad": 1, "wgrad": 2}
+HQ_PRODUCT_KERNEL = ("cuda_cores", "few_rows", "tensor_memory")
+
+
+def linear_plan(product, m, n, k, group, sm_count=148):
+    """hq_linear_plan of these sizes as a dict, `kernel` by name.  Needs neither a GPU nor data."""
+    plan = hq_product_plan()
+    _check(lib().hq_linear_plan(HQ_PRODUCT[product], m, n, k, group, sm_count, C.byref(plan)), "hq_linear_plan")
+    return {**{name: getattr(plan, name) for name, _ in hq_product_plan._fields_}, "kernel": HQ_PRODUCT_KERNEL[plan.kernel]}
 
 
 def conv2d_noalloc(case: dict, dev: dict, out):

@@ -141,6 +141,23 @@ hq_status hq_linear_wgrad8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
   return product(h, PRODUCT_WGRAD, dy->type, a, stream);
 }
 
+hq_status hq_linear_plan(int32_t product, int32_t m, int32_t n, int32_t k, int32_t group, int32_t sm_count, hq_product_plan* plan) {
+  if (product < HQ_PRODUCT_LINEAR || product > HQ_PRODUCT_WGRAD || m < 1 || n < 1 || k < 1 || sm_count < 1 || !plan) return HQ_ERR_INVALID_ARG;
+  if (product != HQ_PRODUCT_WGRAD && (k & 1)) return HQ_ERR_INVALID_ARG;
+  if (group < 32 || group % 32) return HQ_ERR_INVALID_ARG;
+  if (m > kMaxExtent || n > kMaxExtent || k > kMaxExtent) return HQ_ERR_UNSUPPORTED;
+  ProductArgs a{};
+  a.q_cols = k; a.groups = groups_of(k, group); a.group = group;
+  a.i = product == HQ_PRODUCT_LINEAR ? n : k; a.j = product == HQ_PRODUCT_WGRAD ? n : m;
+  a.r = product == HQ_PRODUCT_LINEAR ? k : product == HQ_PRODUCT_DGRAD ? n : m;
+  a.b_stride = product == HQ_PRODUCT_LINEAR ? k : n;
+  *plan = hq_product_plan{};
+  if (product == HQ_PRODUCT_LINEAR && hq_plan_product_few(a, sm_count, plan)) plan->kernel = HQ_KERNEL_FEW_ROWS;
+  else if (hq_plan_product_tc((ProductKind)product, a, sm_count, plan)) plan->kernel = HQ_KERNEL_TENSOR_MEMORY;
+  else plan->kernel = HQ_KERNEL_CUDA_CORES;
+  return HQ_OK;
+}
+
 hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, int32_t act, hq_matrix* y,
                        hq_saved8* saved_x, hq_saved8* saved_gate, void* stream) {
   if (!h || !saved_x || (gate != nullptr) != (saved_gate != nullptr)) return HQ_ERR_INVALID_ARG;

@@ -60,6 +60,9 @@ hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& a, cu
 // On the tensor cores (product_tc.cu): every shape whose rows start on 16 bytes.  hq_launch_product_any takes all of them.
 bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a);
 hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
+// The launch of a shape, for hq_linear_plan; false where the kernel does not take it.
+bool hq_plan_product_few(const ProductArgs& a, int sm_count, hq_product_plan* plan);
+bool hq_plan_product_tc(ProductKind kind, const ProductArgs& a, int sm_count, hq_product_plan* plan);
 cudaError_t hq_launch_product_any(ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
 // Runs `set` the first time for the current device (its kernels' attributes stay set); again after a failure.
 template <class Set>

@@ -538,6 +538,19 @@ bool hq_product_few_supported(const ProductArgs& p, int sm_count) {
   return plan(p, sm_count, a, rt, shared);
 }
 
+bool hq_plan_product_few(const ProductArgs& p, int sm_count, hq_product_plan* out) {
+  if (!hq_product_few_supported(p, sm_count)) return false;
+  FewArgs a{};
+  int rt, shared;
+  plan(p, sm_count, a, rt, shared);
+  const int at_once = (sm_count / a.splits) << (kWarpsLog - a.along_log);
+  out->columns = 8 * columns_eights(p.j, 1 << a.parts_log); out->outputs = kRows * rt; out->splits = a.splits;
+  out->steps = a.range / kStageInputs;
+  out->rounds = (a.tiles + at_once - 1) / at_once;
+  out->stages = a.depth; out->groups = 1 << a.along_log; out->units = 0; out->unit_stages = 0;
+  return true;
+}
+
 hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& p, cudaStream_t s) {
   FewArgs a{};
   int rt = 1, shared = 0;

@@ -41,32 +41,41 @@ __device__ __forceinline__ int converter_number(int warp, bool beside_first) {
   return (beside_first ? 0 : 18) + (warp >> 2) - 4;
 }
 
-// One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages; DGRAD 64 rows of 64 bytes and WGRAD 64
-// rows of 128 bytes, one stage.
-template <int KIND>
+// One fetch of the quantized operand: FORWARD 128 rows of 128 bytes, the inputs of four stages (64 bytes and two stages with 128 columns
+// and more, see Shape); DGRAD 64 rows of 64 bytes and WGRAD 64 rows of 128 bytes, one stage.
+template <int KIND, int NT>
 struct Unit {
-  static constexpr int kStagesOf = KIND == PRODUCT_FORWARD ? 4 : 1;
-  static constexpr int kRowBytes = KIND == PRODUCT_DGRAD ? 64 : 128, kRows = KIND == PRODUCT_FORWARD ? kTileC : kStep;
+  static constexpr int kStagesOf = KIND != PRODUCT_FORWARD ? 1 : NT >= 128 ? 2 : 4;
+  static constexpr int kRowBytes = KIND == PRODUCT_FORWARD ? kStagesOf * kStep / 2 : KIND == PRODUCT_DGRAD ? 64 : 128;
+  static constexpr int kRows = KIND == PRODUCT_FORWARD ? kTileC : kStep;
   static constexpr int kBytes = kRowBytes * kRows;
 };
 // NT = 256: two CTAs of a cluster (neighbouring SMs) share every MMA (cta_group::2), 256 lanes x 256 columns: each converts its own
 // 128 lanes and fetches half of the columns.  One CTA with 256 columns of its own is bound by its shared memory: per stage (512
 // cycles of MMAs) 48 KB go in and 48 KB out beside what the converters move.
 // Converters work in groups, which take the stages in turn (most of a warp's time on one is waiting): two warps with two rows of 64
-// integers per thread, or four with one.  A group may be one round of a ring ahead of another, not two, since a barrier tells a
-// round from the next one only: no more groups than stages in either ring.
+// integers per thread, or four with one.  A barrier tells a round of its ring by its parity, and a wait returns
+// at once while the round before is still under way: whoever waits has to know that the round before is through.
+//   - The ring of the quantized operand: copies land in any order, so a group knows what it has waited for itself and nothing
+//     else.  The ring holds a whole number of turns of the groups: a group then finds its stages in the same places every round.
+//   - The ring of stages is emptied in order.  A group knows that its own last stage, kGroups before the present one, found its place
+//     empty: no more groups than stages.  FORWARD fills a tile's last unit up with stages that nobody converts, so that a group's
+//     last stage may be longer ago; but the unit before in the same place is through, whose last stage is at most a whole ring of the
+//     quantized operand behind: no more of those stages than stages.
 template <int KIND, int NT>
 struct Shape {
   static constexpr bool kPair = NT == 256, kWgrad = KIND == PRODUCT_WGRAD;
   static constexpr int kCtas = kPair ? 2 : 1, kColumnsHere = NT / kCtas;
   static constexpr int kStages = kWgrad ? (NT >= 128 ? 5 : 6) : NT >= 128 ? 6 : 8;
   static constexpr int kStageBytes = kTileABytes + (kColumnsHere < 64 ? 64 : kColumnsHere) * kStep * 2;
-  static constexpr int kRawBytes = (kWgrad ? 48 : 32) * 1024;       // ring of the quantized operand
-  static constexpr int kUnits = kRawBytes / Unit<KIND>::kBytes;
+  static constexpr int kPer = Unit<KIND, NT>::kStagesOf;
+  static constexpr int kUnits = kWgrad ? 8 : kStages / kPer;       // of the ring of the quantized operand: 64 KB, 24 or 32
+  static constexpr int kRawBytes = kUnits * Unit<KIND, NT>::kBytes;
   static constexpr int kSharedBytes = kStages * kStageBytes + kRawBytes + 1024;
   static constexpr int kRowsPerThread = kWgrad ? 1 : 2, kConverterWarps = 4 / kRowsPerThread;
   static constexpr int kGroups = kWgrad ? 4 : kStages;             // (saved activations: five were no faster)
-  static_assert(kGroups <= kStages && kGroups <= Unit<KIND>::kStagesOf * kUnits && kGroups * kConverterWarps <= kMaxConverters && kUnits <= 8 && kStages <= 8);
+  static_assert((kPer * kUnits) % kGroups == 0 && kGroups <= kStages && (kPer == 1 || kPer * kUnits <= kStages));
+  static_assert(kGroups * kConverterWarps <= kMaxConverters && kUnits <= 8 && kStages <= 8);
 };
 
 constexpr int kMaxUnits = 8;
@@ -247,15 +256,15 @@ struct Scales {
 };
 
 // 64 integers of a row of what was fetched (`half`: the half of the lanes, not FORWARD), restored ...
-template <int KIND, class T>
+template <int KIND, class T, int ROW_BYTES>
 __device__ __forceinline__ void convert_row(uint32_t raw, int stage_of_unit, const float (&scale)[2], int row, int half, uint32_t flip, uint32_t (&v)[8][4]) {
   constexpr int kPieces = KIND == PRODUCT_WGRAD ? 4 : 2;           // of 16 bytes
   uint4 q[kPieces];
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int piece = (KIND == PRODUCT_FORWARD ? stage_of_unit * 2 : half * kPieces) + i;
-    const uint32_t swizzled = KIND == PRODUCT_DGRAD ? piece ^ ((row >> 1) & 3) : piece ^ (row & 7);
-    q[i] = load_shared(raw + row * Unit<KIND>::kRowBytes + (swizzled << 4));
+    const uint32_t swizzled = ROW_BYTES == 64 ? piece ^ ((row >> 1) & 3) : piece ^ (row & 7);
+    q[i] = load_shared(raw + row * ROW_BYTES + (swizzled << 4));
   }
   const uint32_t* w = (const uint32_t*)q;
 #pragma unroll
@@ -286,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
   constexpr int kBoxes = KIND == PRODUCT_WGRAD ? (kColumnsHere + 63) / 64 : 1;
   constexpr int kBBytes = KIND == PRODUCT_WGRAD ? kBoxes * 64 * kStep * 2 : kColumnsHere * kStep * 2;     // that a CTA's copies bring per stage
   constexpr uint32_t kColumns = NT * 2;
-  constexpr int kPer = Unit<KIND>::kStagesOf, kUnits = Shape<KIND, NT>::kUnits, kRowsPerThread = Shape<KIND, NT>::kRowsPerThread;
+  constexpr int kPer = Shape<KIND, NT>::kPer, kUnits = Shape<KIND, NT>::kUnits, kRowsPerThread = Shape<KIND, NT>::kRowsPerThread;
   constexpr int kConverterWarps = Shape<KIND, NT>::kConverterWarps;
   const uint32_t base = (smem_u32(raw_shared) + 1023u) & ~1023u, raw_ring = base + kStages * kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -330,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       // the quantized operand of stages `st` and on
       auto fetch_unit = [&](int i0, int st) {
         if (!mbar_wait(smem_u32(&ctl.raw_empty[u]), u_phase ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER)) return false;
-        const uint32_t bar = smem_u32(&ctl.raw_full[u]), dst = raw_ring + u * Unit<KIND>::kBytes;
-        mbar_expect_tx(bar, Unit<KIND>::kBytes);
+        const uint32_t bar = smem_u32(&ctl.raw_full[u]), dst = raw_ring + u * Unit<KIND, NT>::kBytes;
+        mbar_expect_tx(bar, Unit<KIND, NT>::kBytes);
         if (KIND == PRODUCT_FORWARD) tma_load_2d(dst, &map_q, bar, st * (kStep / 2), i0);
         else tma_load_2d(dst, &map_q, bar, KIND == PRODUCT_DGRAD ? i0 >> 1 : i0, st * kStep);
         u_issued |= 1u << u;
@@ -441,16 +450,16 @@ __global__ void __launch_bounds__(kThreads, 1) product_tc_kernel(const __grid_co
       const unsigned n = before + st, v = before_padded + st, unit_no = v / kPer;
       const bool real = st < steps;
       const int u = unit_no % kUnits, s = (int)(n % kStages);
-      const uint32_t raw = raw_ring + u * Unit<KIND>::kBytes, to = base + s * kStageBytes;
+      const uint32_t raw = raw_ring + u * Unit<KIND, NT>::kBytes, to = base + s * kStageBytes;
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.raw_full[u]), (unit_no / kUnits) & 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) break;
       if (real) {
         // the first row's values are made before the stage they go to is free
         uint32_t value[8][4];
-        convert_row<KIND, T>(raw, (int)(v % kPer), scale[0], row0, half, flip, value);
+        convert_row<KIND, T, Unit<KIND, NT>::kRowBytes>(raw, (int)(v % kPer), scale[0], row0, half, flip, value);
         if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.empty[s]), ((n / kStages) & 1) ^ 1, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) break;
         store_row(to, row0, half, value);
         if (kRowsPerThread == 2) {
-          convert_row<KIND, T>(raw, (int)(v % kPer), scale[kRowsPerThread - 1], row0 + 32, half, flip, value);
+          convert_row<KIND, T, Unit<KIND, NT>::kRowBytes>(raw, (int)(v % kPer), scale[kRowsPerThread - 1], row0 + 32, half, flip, value);
           store_row(to, row0 + 32, half, value);
         }
         fence_async_smem();
@@ -597,13 +606,23 @@ bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a) {
   return kind == PRODUCT_WGRAD ? a.q_cols % 16 == 0 : a.q_cols % 32 == 0;  // and so do those of the quantized operand
 }
 
-hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const ProductArgs& p, cudaStream_t s) {
-  TcArgs a{};
-  a.p = p;
-  a.status = h->dev_status;
+namespace {
+
+template <int KIND, int NT>
+void fill_rings(hq_product_plan* plan) {
+  using S = Shape<KIND, NT>;
+  plan->stages = S::kStages; plan->groups = S::kGroups; plan->units = S::kUnits; plan->unit_stages = S::kPer;
+}
+template <int KIND>
+void fill_rings(int nt, hq_product_plan* plan) {
+  nt == 32 ? fill_rings<KIND, 32>(plan) : nt == 64 ? fill_rings<KIND, 64>(plan) : nt == 128 ? fill_rings<KIND, 128>(plan) : fill_rings<KIND, 256>(plan);
+}
+
+// Columns per tile and CTAs (or pairs) per tile: what is through first, by the cycles that a stage, a tile and the joining of parts
+// take (a stage, counted in the kernel: 650 with 256 columns on a pair, about 600 with 64, 32 and with saved activations).
+// Returns the columns, 0 for more tiles than can be counted.
+int plan_tiles(const ProductArgs& p, int sm_count, TcArgs& a) {
   a.steps = (p.r + kStep - 1) / kStep;
-  // Columns per tile and CTAs (or pairs) per tile: what is through first, by the cycles that a stage, a tile and the joining of parts
-  // take (a stage, counted in the kernel: 650 with 256 columns on a pair, about 600 with 64, 32 and with saved activations).
   int nt = 0;
   long long best = 0;
   for (const int width : {32, 64, 128, 256}) {
@@ -613,7 +632,7 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
     for (int splits = 1; splits * ctas <= 8; splits *= 2) {
       const int split_steps = (a.steps + splits - 1) / splits;
       if (splits > 1 && ((splits - 1) * split_steps >= a.steps || split_steps < 4)) break;
-      const long long at_once = h->sm_count / (ctas * splits);
+      const long long at_once = sm_count / (ctas * splits);
       if (at_once < 1) break;
       const long long rounds = (tiles + at_once - 1) / at_once;
       if (splits > 1 && rounds > 1) break;
@@ -623,7 +642,29 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
       a.i_tiles = (int)i_tiles; a.tiles = (int)tiles; a.splits = splits; a.split_steps = split_steps;
     }
   }
+  return nt;
+}
+
+}  // namespace
+
+bool hq_plan_product_tc(ProductKind kind, const ProductArgs& p, int sm_count, hq_product_plan* plan) {
+  if (!hq_product_tc_supported(kind, p)) return false;
+  TcArgs a{};
+  const int nt = plan_tiles(p, sm_count, a);
+  if (nt == 0) return false;
+  kind == PRODUCT_FORWARD ? fill_rings<PRODUCT_FORWARD>(nt, plan) : kind == PRODUCT_DGRAD ? fill_rings<PRODUCT_DGRAD>(nt, plan) : fill_rings<PRODUCT_WGRAD>(nt, plan);
+  const int at_once = sm_count / ((nt == 256 ? 2 : 1) * a.splits);
+  plan->columns = nt; plan->outputs = (nt == 256 ? 2 : 1) * kTileC; plan->splits = a.splits; plan->steps = a.split_steps;
+  plan->rounds = (a.tiles + at_once - 1) / at_once;
+  return true;
+}
+
+hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const ProductArgs& p, cudaStream_t s) {
+  TcArgs a{};
+  const int nt = plan_tiles(p, h->sm_count, a);
   if (nt == 0) return HQ_ERR_UNSUPPORTED;
+  a.p = p;
+  a.status = h->dev_status;
   const int ctas = nt == 256 ? 2 : 1, at_once = h->sm_count / ctas;
   const int grid = (a.splits > 1 ? a.tiles * a.splits : a.tiles < at_once ? a.tiles : at_once) * ctas;
   // k / group by a multiply-high, exact while (k / 32) (group / 32) < 2^31
@@ -633,7 +674,9 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
   }
   CUtensorMap map[2];
   const bool bytes = kind == PRODUCT_WGRAD;
-  const int unit_row = kind == PRODUCT_DGRAD ? Unit<PRODUCT_DGRAD>::kRowBytes : 128, unit_rows = kind == PRODUCT_FORWARD ? kTileC : kStep;
+  const int unit_row = kind == PRODUCT_WGRAD ? Unit<PRODUCT_WGRAD, 32>::kRowBytes : kind == PRODUCT_DGRAD ? Unit<PRODUCT_DGRAD, 32>::kRowBytes
+                     : nt >= 128 ? Unit<PRODUCT_FORWARD, 128>::kRowBytes : Unit<PRODUCT_FORWARD, 32>::kRowBytes;
+  const int unit_rows = kind == PRODUCT_FORWARD ? kTileC : kStep;
   if (!encode_rows_map(&map[0], p.q, kind == PRODUCT_FORWARD ? p.i : p.r, bytes ? p.q_cols : p.q_cols >> 1, unit_row, unit_rows, swizzle_for(unit_row)) ||
       !encode_b_map(&map[1], type, p, kind, nt)) return HQ_ERR_CUDA;
   const cudaError_t e = type == HQ_F16 ? launch_kind<__half>(kind, nt, map, a, grid, s) : launch_kind<__nv_bfloat16>(kind, nt, map, a, grid, s);
