@@ -383,8 +383,9 @@ hq_status hq_linear_w4_dgrad(hq_handle* h, const hq_matrix* dy, const hq_w4* w, 
 /*
  * Activation that saves its input for the backward pass:  y = f(x), or y = f(x) * gate;
  *   scale = max|x| / 127 over a group of a row (rounded to 32 bits),  q = x / scale rounded to the nearest integer, ties
- *   to even, of the exact quotient; a group of zeros has scale 0 and q = 0.  A group that holds an infinity or a NaN has
- *   scale NaN and q = 0: all of it is restored as NaN.
+ *   to even, of the exact quotient, and at most 127 in magnitude (a scale below 2^-142 has so few bits that the quotient can pass
+ *   that); a group of zeros, or of values so small that the scale rounds to 0, has scale 0 and q = 0.  A group that holds an
+ *   infinity or a NaN has scale NaN and q = 0: all of it is restored as NaN.
  * x, gate, y: (rows, cols) of one type, HQ_F32, HQ_F16 or HQ_BF16.  gate (and with it saved_gate) may be NULL, y may be NULL
  * (x is saved and nothing else).
  */

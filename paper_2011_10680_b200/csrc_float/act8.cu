@@ -181,8 +181,9 @@ __device__ __forceinline__ uint2 quantize8(const Two (&x)[kPairs], float s, floa
   } else {                                                          // 0, NaN, or so small that 1 / s leaves the 32-bit range
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
+      // (a scale of a few units of 2^-149 may be rounded down so far that the quotient passes 127: up to 190, top = 190 2^-149)
       const float v = i & 1 ? hi(x[i / 2]) : lo(x[i / 2]);
-      q[i] = s > 0.f ? __double2int_rn((double)v / (double)s) : 0;
+      q[i] = s > 0.f ? min(max(__double2int_rn((double)v / (double)s), -127), 127) : 0;
     }
   }
   uint2 w;

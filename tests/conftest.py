@@ -12,6 +12,22 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a CUDA device (run with -m gpu on a B200)")
 
 
+# Tests that hold a wrong value.  They stay as they are and run; the test named beside each holds the right one.
+WRONG_VALUES = {
+    # 32-bit groups whose largest magnitude is 2^-142 .. 2^-137 have a scale of 1 .. 32 units of 2^-149 (2^7 / 127 = 1.008 .. 2^12 / 127 =
+    # 32.25, rounded), so the quotient is 128, which the test's cast to 8 bits turns into -128: a largest value restored with the
+    # other sign.
+    "test_gpu_float_ops.py::test_act_every_rounding_border[dtype2]": "128 wrapped to -128; see test_gpu_float_limits.py::test_act_rounding_borders",
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        for name, reason in WRONG_VALUES.items():
+            if item.nodeid.endswith(name):
+                item.add_marker(pytest.mark.xfail(reason=reason, strict=True))
+
+
 @pytest.fixture(scope="session")
 def golden_dir():
     return os.path.join(ROOT, "tests", "golden")
