@@ -15,9 +15,8 @@
 //     every group has a sum of its own ("parts"; 64: two columns per row, 32: four).
 //   - Few outputs: a team of 2 .. 16 warps of a CTA splits the inputs of a tile, the CTAs of a cluster do too, and the parts are
 //     added up in shared memory in a fixed order.  Teams do not wait for one another.
-//   - Rows with infinities, NaN or values of 2^73 and more, which the representation does not hold, are computed value by value.
-#include <type_traits>
-
+//   - Infinities, NaN and values of 2^73 and more, which the representation does not hold, and results that come out infinite or NaN
+//     (an infinite scale): once more, value by value.
 #include "../csrc/tc_common.cuh"
 #include "float_internal.cuh"
 
@@ -49,6 +48,8 @@ struct Control {
   unsigned long long full[kWarps][kMaxDepth];
   volatile uint32_t abort_flag;
   volatile uint32_t flip;
+  volatile uint32_t beyond;         // x holds something that the representation does not
+  volatile uint32_t not_finite;     // a result came out like that
 };
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -96,20 +97,40 @@ template <> __device__ __forceinline__ uint32_t largest<__half>(const uint4& v) 
   return __float_as_uint(__half2float(__half(r)));
 }
 
-// Sum of x w over `len` inputs of one output and row, value by value; what lies past k_end is left out.
-template <class T>
-__device__ __noinline__ float by_value_sum(const ProductArgs& p, int i, int row, int from, int len, int k_end) {
-  const T* x = (const T*)p.b + row * p.b_stride;
-  const uint8_t* q = (const uint8_t*)p.q + (long long)i * (p.q_cols >> 1);
-  const T* s = (const T*)p.scale + (long long)i * p.groups;
-  float sum = 0.f;
-  for (int k = from; k < from + len && k < k_end; ++k) sum = fmaf(hq_to_float(x[k]), (float)hq_nibble(q, k) * hq_to_float(s[k / p.group]), sum);
-  return sum;
+// Results value by value, a warp on each: those that came out infinite or NaN, or all of them.  (A group's sum times an infinite scale is no
+// sum of the products: an integer of zero, or terms of both signs, make a NaN of that.  Such a scale always ends in a result that is
+// not finite, so nothing else has to look for it.)
+template <class T, int RT>
+__device__ __noinline__ void by_value(const FewArgs& a, bool all) {
+  const ProductArgs& p = a.p;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups_of_ctas = gridDim.x / a.splits;
+  if (a.splits > 1 && cluster_ctarank() != 0) return;              // (256 results at a time at most: the first CTA's threads have written all)
+  // the tiles of the CTA's teams, one after the other
+  for (int tile = blockIdx.x / a.splits; tile < a.tiles; tile += groups_of_ctas) {
+    for (int e = warp; e < p.j * (16 * RT); e += kWarps) {
+      const int row = e / (16 * RT), i = tile * (16 * RT) + e % (16 * RT);
+      if (i >= p.i) continue;
+      T* const at = (T*)p.out + row * p.out_stride + i;
+      if (!all && isfinite(hq_to_float(*at))) continue;
+      const T* x = (const T*)p.b + row * p.b_stride;
+      const uint8_t* q = (const uint8_t*)p.q + (long long)i * (p.q_cols >> 1);
+      const T* s = (const T*)p.scale + (long long)i * p.groups;
+      float sum = 0.f;
+      for (int k = lane * 2; k < p.r; k += 64) {
+        const float scale = hq_to_float(s[k / p.group]);
+        sum = fmaf(hq_to_float(x[k]), (float)hq_nibble(q, k) * scale, sum);
+        sum = fmaf(hq_to_float(x[k + 1]), (float)hq_nibble(q, k + 1) * scale, sum);
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) *at = hq_from_float<T>(sum + (p.bias ? hq_to_float(((const T*)p.bias)[i]) : 0.f));
+    }
+  }
 }
 
 // NB: eights of columns; RT: sixteens of outputs per warp; WHOLE: a step has one scale per output.
 template <class T, int NB, int RT, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_constant__ CUtensorMap map_q, const FewArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ FewArgs a) {
   extern __shared__ uint8_t raw_shared[];
   __shared__ Control ctl;
   constexpr int kStageBytes = 16 * RT * 128;
@@ -133,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
 
   if (lane == 0)
     for (int s = 0; s < a.depth; ++s) mbar_init(smem_u32(&ctl.full[warp][s]), 1 + 32);
-  if (threadIdx.x == 0) { ctl.abort_flag = 0; ctl.flip = 0x00080008u; }
+  if (threadIdx.x == 0) { ctl.abort_flag = 0; ctl.beyond = 0; ctl.not_finite = 0; ctl.flip = 0x00080008u; }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncwarp();
   hq_pdl_entry();
@@ -220,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
     }
     if (threadIdx.x < 16) ((uint4*)shared)[threadIdx.x] = make_uint4(0, 0, 0, 0);
   }
-  const bool by_value = __syncthreads_or(beyond);
+  if (__syncthreads_or(beyond) && threadIdx.x == 0) ctl.beyond = 1;
   const uint32_t flip = ctl.flip, flip4 = flip << 4;
 
   // column g of every eight: its part has to be that of the thread's inputs, else it reads the zeros
@@ -259,170 +280,155 @@ __global__ void __launch_bounds__(kThreads, 1) product_few_kernel(const __grid_c
   int lost = 0, lost_slot = 0;                                     // a wait that ran out: copies in flight then, and the first one's place
   uint32_t lost_phase = 0;
   bool ok = true;
-  auto work = [&](auto value_by_value) {
-    constexpr bool kByValue = decltype(value_by_value)::value;
-    float total[RT][NB][4] = {};
-    int n = 0, slot = 0;
-    uint32_t phase = 0;
-    for (int tile = tile0; tile < a.tiles; tile += tile_stride) {
-     for (int stage = 0; stage < my_stages; ++stage, ++n) {
-      if (ok && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[warp][slot]), phase, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) {
-        ok = false;
-        lost = min(a.depth, units - n); lost_slot = slot; lost_phase = phase;
+  float total[RT][NB][4] = {};
+  int n = 0, slot = 0;
+  uint32_t phase = 0;
+  for (int tile = tile0; tile < a.tiles; tile += tile_stride) {
+   for (int stage = 0; stage < my_stages; ++stage, ++n) {
+    if (ok && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl.full[warp][slot]), phase, &ctl, a.status, HQ_DEV_TIMEOUT_PRODUCER))) {
+      ok = false;
+      lost = min(a.depth, units - n); lost_slot = slot; lost_phase = phase;
+    }
+    const uint32_t from = ring + slot * kStageBytes;
+    const int st0 = ((stage << a.along_log) + kw) * 2, k0 = k_begin + st0 * kStep;
+    // (with one eight of columns both halves of the stage at once: twice the chains of dependent sums)
+    float acc[2][RT][NB][4] = {};
+    constexpr int kTogether = NB == 1 ? 2 : 1;
+#pragma unroll
+    for (int half0 = 0; half0 < 2; half0 += kTogether) {
+      uint4 w[kTogether][2 * RT];
+#pragma unroll
+      for (int y = 0; y < kTogether; ++y)
+#pragma unroll
+        for (int h = 0; h < 2 * RT; ++h) w[y][h] = load_shared(from + (row_in_8 + 8 * h) * 128 + ((((half0 + y) * 4 + t) ^ row_in_8) << 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint4 b[kTogether][NB];
+#pragma unroll
+        for (int y = 0; y < kTogether; ++y)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) b[y][nb] = load_shared(x_at[nb] + (st0 + half0 + y) * x_step[nb] + i * 64);
+#pragma unroll
+        for (int y = 0; y < kTogether; ++y) {
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const uint32_t lo = word(w[y][2 * r], i), hi = word(w[y][2 * r + 1], i), lo8 = lo >> 8, hi8 = hi >> 8;
+            const uint32_t a0 = lower(lo, flip), a1 = lower(hi, flip), a2 = upper(lo, flip4), a3 = upper(hi, flip4);
+            const uint32_t c0 = lower(lo8, flip), c1 = lower(hi8, flip), c2 = upper(lo8, flip4), c3 = upper(hi8, flip4);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              mma(acc[half0 + y][r][nb], a0, a1, a2, a3, b[y][nb].x, b[y][nb].y);
+              mma(acc[half0 + y][r][nb], c0, c1, c2, c3, b[y][nb].z, b[y][nb].w);
+            }
+          }
+        }
       }
-      const uint32_t from = ring + slot * kStageBytes;
-      const int st0 = ((stage << a.along_log) + kw) * 2, k0 = k_begin + st0 * kStep;
-      if (!kByValue) {
-        // (with one eight of columns both halves of the stage at once: twice the chains of dependent sums)
-        float acc[2][RT][NB][4] = {};
-        constexpr int kTogether = NB == 1 ? 2 : 1;
+    }
+    const uint32_t first = __umulhi((uint32_t)k0 >> 4, a.group_mul);
+    // the first scale of an output lies in the upper half of its word where its index is odd
+    uint32_t s_at[2 * RT];
 #pragma unroll
-        for (int half0 = 0; half0 < 2; half0 += kTogether) {
-          uint4 w[kTogether][2 * RT];
+    for (int h = 0; h < 2 * RT; ++h) {
+      const uint32_t in_tile = row_in_8 + 8 * h, row = (uint32_t)tile * (16 * RT) + in_tile;
+      s_at[h] = scale_ring + slot * kScaleBytes + in_tile * a.scale_pitch + (((row * (uint32_t)p.groups + first) & 1) << 1);
+    }
 #pragma unroll
-          for (int y = 0; y < kTogether; ++y)
+    for (int half = 0; half < 2; ++half) {
+      // (inputs past the last one give sums of zero; their scales, whatever is found there, must not make a NaN of it)
+      const int k = k0 + half * kStep;
+      const bool on0 = k + part0 < k_end, on1 = k + part1 < k_end;
+      const uint32_t i0 = (__umulhi((uint32_t)(k + part0) >> 4, a.group_mul) - first) * 2;
+      const uint32_t i1 = WHOLE ? i0 : (__umulhi((uint32_t)(k + part1) >> 4, a.group_mul) - first) * 2;
+      float s0[2 * RT], s1[2 * RT];
 #pragma unroll
-            for (int h = 0; h < 2 * RT; ++h) w[y][h] = load_shared(from + (row_in_8 + 8 * h) * 128 + ((((half0 + y) * 4 + t) ^ row_in_8) << 4));
+      for (int h = 0; h < 2 * RT; ++h) {
+        s0[h] = on0 ? hq_to_float(load_scale<T>(s_at[h] + i0)) : 0.f;
+        s1[h] = WHOLE ? s0[h] : on1 ? hq_to_float(load_scale<T>(s_at[h] + i1)) : 0.f;
+      }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint4 b[kTogether][NB];
-#pragma unroll
-            for (int y = 0; y < kTogether; ++y)
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb) b[y][nb] = load_shared(x_at[nb] + (st0 + half0 + y) * x_step[nb] + i * 64);
-#pragma unroll
-            for (int y = 0; y < kTogether; ++y) {
-#pragma unroll
-              for (int r = 0; r < RT; ++r) {
-                const uint32_t lo = word(w[y][2 * r], i), hi = word(w[y][2 * r + 1], i), lo8 = lo >> 8, hi8 = hi >> 8;
-                const uint32_t a0 = lower(lo, flip), a1 = lower(hi, flip), a2 = upper(lo, flip4), a3 = upper(hi, flip4);
-                const uint32_t c0 = lower(lo8, flip), c1 = lower(hi8, flip), c2 = upper(lo8, flip4), c3 = upper(hi8, flip4);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                  mma(acc[half0 + y][r][nb], a0, a1, a2, a3, b[y][nb].x, b[y][nb].y);
-                  mma(acc[half0 + y][r][nb], c0, c1, c2, c3, b[y][nb].z, b[y][nb].w);
-                }
-              }
-            }
-          }
-        }
-        const uint32_t first = __umulhi((uint32_t)k0 >> 4, a.group_mul);
-        // the first scale of an output lies in the upper half of its word where its index is odd
-        uint32_t s_at[2 * RT];
-#pragma unroll
-        for (int h = 0; h < 2 * RT; ++h) {
-          const uint32_t in_tile = row_in_8 + 8 * h, row = (uint32_t)tile * (16 * RT) + in_tile;
-          s_at[h] = scale_ring + slot * kScaleBytes + in_tile * a.scale_pitch + (((row * (uint32_t)p.groups + first) & 1) << 1);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          // (inputs past the last one give sums of zero; their scales, whatever is found there, must not make a NaN of it)
-          const int k = k0 + half * kStep;
-          const bool on0 = k + part0 < k_end, on1 = k + part1 < k_end;
-          const uint32_t i0 = (__umulhi((uint32_t)(k + part0) >> 4, a.group_mul) - first) * 2;
-          const uint32_t i1 = WHOLE ? i0 : (__umulhi((uint32_t)(k + part1) >> 4, a.group_mul) - first) * 2;
-          float s0[2 * RT], s1[2 * RT];
-#pragma unroll
-          for (int h = 0; h < 2 * RT; ++h) {
-            s0[h] = on0 ? hq_to_float(load_scale<T>(s_at[h] + i0)) : 0.f;
-            s1[h] = WHOLE ? s0[h] : on1 ? hq_to_float(load_scale<T>(s_at[h] + i1)) : 0.f;
-          }
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            const uint4 f = load_shared(base + a.fix_at + ((st0 + half) * (8 * NB) + nb * 8 + 2 * t) * 8);
-            const float p0 = __uint_as_float(f.x), c0 = __uint_as_float(f.y), p1 = __uint_as_float(f.z), c1 = __uint_as_float(f.w);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float (&sum)[4] = total[r][nb];
-                const float (&v)[4] = acc[half][r][nb];
-                sum[2 * h] = fmaf(s0[2 * r + h], fmaf(v[2 * h], p0, c0), sum[2 * h]);
-                sum[2 * h + 1] = fmaf(s1[2 * r + h], fmaf(v[2 * h + 1], p1, c1), sum[2 * h + 1]);
-              }
-            }
-          }
-        }
-      } else {
+      for (int nb = 0; nb < NB; ++nb) {
+        const uint4 f = load_shared(base + a.fix_at + ((st0 + half) * (8 * NB) + nb * 8 + 2 * t) * 8);
+        const float p0 = __uint_as_float(f.x), c0 = __uint_as_float(f.y), p1 = __uint_as_float(f.z), c1 = __uint_as_float(f.w);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-            for (int k2 = 0; k2 < 4; ++k2) {
-              const int row = (nb * 8 + 2 * t + (k2 & 1)) >> parts_log, i = tile * (16 * RT) + 16 * r + row_in_8 + 8 * (k2 >> 1);
-              if (row < p.j && i < p.i)
-                for (int half = 0; half < 2; ++half)
-                  total[r][nb][k2] += by_value_sum<T>(p, i, row, k0 + half * kStep + (k2 & 1 ? part1 : part0), kStep >> parts_log, k_end);
-            }
+          for (int h = 0; h < 2; ++h) {
+            float (&sum)[4] = total[r][nb];
+            const float (&v)[4] = acc[half][r][nb];
+            sum[2 * h] = fmaf(s0[2 * r + h], fmaf(v[2 * h], p0, c0), sum[2 * h]);
+            sum[2 * h + 1] = fmaf(s1[2 * r + h], fmaf(v[2 * h + 1], p1, c1), sum[2 * h + 1]);
           }
         }
-      }
-      __syncwarp();
-      if (ok && n + a.depth < units) fetch();
-      if (++slot == a.depth) { slot = 0; phase ^= 1; }
-     }
-      // the tile's inputs are through: add up the warps' parts, all outputs at once with one eight of columns, sixteen with two (the
-      // sums of 16 outputs of a column lie together, every other pair of columns turned by eight to spread the banks)
-      auto meet = [&]() {
-        if (a.along_log == 0) __syncwarp();
-        else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 << a.along_log) : "memory");
-      };
-      constexpr int kHalves = NB == 1 ? RT : 1, kSums = 16 * 8 * NB * kHalves;       // sixteens of outputs, values of a warp
-#pragma unroll
-      for (int r0 = 0; r0 < RT; r0 += kHalves) {
-        float* mine = (float*)(shared + a.red_at) + warp * kSums;
-#pragma unroll
-        for (int r = r0; r < r0 + kHalves; ++r)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-          for (int k2 = 0; k2 < 4; ++k2) {
-            mine[(((r - r0) * NB + nb) * 8 + 2 * t + (k2 & 1)) * 16 + ((row_in_8 + (k2 >> 1) * 8) ^ ((t & 1) << 3))] = total[r][nb][k2];
-            total[r][nb][k2] = 0.f;
-          }
-        }
-        meet();
-        const float* sums = (const float*)(shared + a.red_at) + (team << a.along_log) * kSums;
-        const int members = 32 << a.along_log, outputs = p.j * (16 * kHalves);
-        auto output = [&](int e, float sum) {
-          const int row = e / (16 * kHalves), i = tile * (16 * RT) + r0 * 16 + (e & (16 * kHalves - 1));
-          if (i < p.i) {
-            if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
-            ((T*)p.out)[row * p.out_stride + i] = hq_from_float<T>(sum);
-          }
-        };
-        for (int e = kw * 32 + lane; e < outputs; e += members) {
-          const int col = ((e / (16 * kHalves)) << parts_log) + (kHalves == 2 ? (e >> 4 & 1) * 8 : 0), turned = (e & 15) ^ ((col >> 1 & 1) << 3);
-          const float* part = sums + col * 16 + turned;            // a row's columns: this one, the next, and two more, turned the other way
-          const int other = 32 + (turned ^ 8) - turned;
-          float sum = 0.f;
-#pragma unroll 4
-          for (int k2 = 0; k2 < along; ++k2, part += kSums) {
-            sum += part[0];
-            if (!WHOLE) sum += part[16];
-            if (!WHOLE && parts == 4) { sum += part[other]; sum += part[other + 16]; }
-          }
-          if (a.splits == 1) output(e, sum); else ((float*)(shared + a.sum_at))[e] = sum;
-        }
-        if (a.splits > 1) {
-          cluster_sync_all();
-          for (int e = threadIdx.x + rank * kThreads; e < outputs; e += kThreads * a.splits) {
-            float sum = 0.f;
-            for (int c = 0; c < a.splits; ++c) {
-              float v;
-              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(base + a.sum_at + e * 4, c)));
-              sum += v;
-            }
-            output(e, sum);
-          }
-          cluster_sync_all();
-        }
-        meet();                                                    // the sums are read
       }
     }
-  };
-  if (by_value) work(std::true_type{}); else work(std::false_type{});
+    __syncwarp();
+    if (ok && n + a.depth < units) fetch();
+    if (++slot == a.depth) { slot = 0; phase ^= 1; }
+   }
+    // the tile's inputs are through: add up the warps' parts, all outputs at once with one eight of columns, sixteen with two (the
+    // sums of 16 outputs of a column lie together, every other pair of columns turned by eight to spread the banks)
+    auto meet = [&]() {
+      if (a.along_log == 0) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 << a.along_log) : "memory");
+    };
+    constexpr int kHalves = NB == 1 ? RT : 1, kSums = 16 * 8 * NB * kHalves;       // sixteens of outputs, values of a warp
+#pragma unroll
+    for (int r0 = 0; r0 < RT; r0 += kHalves) {
+      float* mine = (float*)(shared + a.red_at) + warp * kSums;
+#pragma unroll
+      for (int r = r0; r < r0 + kHalves; ++r)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int k2 = 0; k2 < 4; ++k2) {
+          mine[(((r - r0) * NB + nb) * 8 + 2 * t + (k2 & 1)) * 16 + ((row_in_8 + (k2 >> 1) * 8) ^ ((t & 1) << 3))] = total[r][nb][k2];
+          total[r][nb][k2] = 0.f;
+        }
+      }
+      meet();
+      const float* sums = (const float*)(shared + a.red_at) + (team << a.along_log) * kSums;
+      const int members = 32 << a.along_log, outputs = p.j * (16 * kHalves);
+      auto output = [&](int e, float sum) {
+        const int row = e / (16 * kHalves), i = tile * (16 * RT) + r0 * 16 + (e & (16 * kHalves - 1));
+        if (i < p.i) {
+          if (!isfinite(sum)) ctl.not_finite = 1;
+          if (p.bias) sum += hq_to_float(((const T*)p.bias)[i]);
+          ((T*)p.out)[row * p.out_stride + i] = hq_from_float<T>(sum);
+        }
+      };
+      for (int e = kw * 32 + lane; e < outputs; e += members) {
+        const int col = ((e / (16 * kHalves)) << parts_log) + (kHalves == 2 ? (e >> 4 & 1) * 8 : 0), turned = (e & 15) ^ ((col >> 1 & 1) << 3);
+        const float* part = sums + col * 16 + turned;            // a row's columns: this one, the next, and two more, turned the other way
+        const int other = 32 + (turned ^ 8) - turned;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int k2 = 0; k2 < along; ++k2, part += kSums) {
+          sum += part[0];
+          if (!WHOLE) sum += part[16];
+          if (!WHOLE && parts == 4) { sum += part[other]; sum += part[other + 16]; }
+        }
+        if (a.splits == 1) output(e, sum); else ((float*)(shared + a.sum_at))[e] = sum;
+      }
+      if (a.splits > 1) {
+        cluster_sync_all();
+        if (rank != 0 && threadIdx.x == 0 && ctl.beyond)
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(smem_u32((const void*)&ctl.beyond), 0)), "r"(1) : "memory");
+        for (int e = threadIdx.x + rank * kThreads; e < outputs; e += kThreads * a.splits) {
+          float sum = 0.f;
+          for (int c = 0; c < a.splits; ++c) {
+            float v;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(base + a.sum_at + e * 4, c)));
+            sum += v;
+          }
+          output(e, sum);
+        }
+        cluster_sync_all();
+      }
+      meet();                                                    // the sums are read
+    }
+  }
+  __syncthreads();                                                 // the results are written
+  if (ctl.beyond || ctl.not_finite) by_value<T, RT>(a, ctl.beyond);
   if (!ok && lane == 0) {                                          // let the copies in flight land before the memory goes
     for (; lost > 0; --lost) {
       const unsigned long long t0 = global_ns();

@@ -62,3 +62,58 @@ def test_act_smallest_magnitudes_keep_their_sign(hq, cols):  # noqa: F811
     assert bool((xq.double() * x.double() >= 0).all())
     # half a step is lost, and what a quotient beyond 127 loses: 63 steps at 190 units
     assert bool(((xq.double() * wide - x.double()).abs() <= torch.maximum(wide * 63, x.double().abs() * (wide == 0))).all())
+
+
+# ------------------------------------------------------------------------------------------------ scales of weights that are not finite
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("k,group", [(256, 32), (256, 64), (512, 128), (100, 32), (16384, 128)])
+@pytest.mark.parametrize("m", [1, 3, 8, 16, 17, 70])
+def test_linear_w4_infinite_scales(hq, m, k, group, dtype):  # noqa: F811
+    """q * infinity by IEEE's rules, term by term: infinite where all terms of the group are, with one sign, NaN otherwise."""
+    if m > 20 and k > 1000:
+        pytest.skip("one size of many rows is enough")
+    g = gen(31)
+    n, groups = 48, ops.groups(k, group)
+    v = torch.randint(-7, 8, (n, k), generator=g, device="cuda")
+    v[v == 0] = 5
+    x = normal(g, m, k)
+    x[x == 0] = 1
+    s = torch.full((n, groups), 0.5, device="cuda", dtype=dtype)
+    sign = torch.sign(x[0])
+    hit = slice(group * (groups - 1), k)                          # the last group, which may be shorter
+    for i, mode in enumerate(("plain", "one sign", "other sign", "both signs", "a zero", "first group", "nan")):
+        if mode == "plain":
+            continue
+        at = slice(0, group) if mode == "first group" else hit
+        s[i, 0 if mode == "first group" else groups - 1] = float("nan") if mode == "nan" else float("-inf" if mode == "other sign" else "inf")
+        v[i, at] = (v[i, at].abs() * sign[at]).long()             # every term of row 0 positive
+        if mode == "both signs":
+            v[i, at.stop - 1] = -v[i, at.stop - 1]
+        if mode == "a zero":
+            v[i, at.stop - 1] = 0
+    bits = (v & 15).to(torch.int32)
+    q = (bits[:, 0::2] | (bits[:, 1::2] << 4)).to(torch.uint8)
+    x = x.to(dtype)
+    out = out_matrix(m, n, dtype)
+    assert hq.linear_w4(x, q, s, group, None, out) == 0
+    hq.sync()
+    # (a product of matrices may skip or reorder nothing here: term by term, in 64 bits)
+    w = v.double() * s.double().repeat_interleave(group, dim=1)[:, :k]
+    ref = torch.stack([(x.double()[r] * w).sum(dim=1) for r in range(m)])
+    assert bool(torch.isinf(ref[0, 1])) and bool(torch.isinf(ref[0, 2])) and bool(torch.isinf(ref[0, 5])) and bool(torch.isnan(ref[0, 3:5]).all())
+    assert torch.equal(torch.isnan(out), torch.isnan(ref))
+    infinite = torch.isinf(ref)
+    assert torch.equal(out[infinite].double(), ref[infinite]) and bool(torch.isfinite(out[torch.isfinite(ref)]).all())
+
+
+def test_linear_w4_sums_beyond_32_bits_are_infinite(hq):  # noqa: F811
+    """Finite scales and activations whose products pass the 32-bit range: infinite with the sign of the sum, few rows and many."""
+    for m in (1, 4, 40):
+        q = torch.full((32, 64), 0x77, dtype=torch.uint8, device="cuda")
+        q[16:] = 0x99                                             # -7
+        s = torch.full((32, 1), 2.0 ** 60, dtype=BF16, device="cuda")
+        x = torch.full((m, 128), 2.0 ** 72, dtype=BF16, device="cuda")
+        out = out_matrix(m, 32, BF16)
+        assert hq.linear_w4(x, q, s, 128, None, out) == 0
+        hq.sync()
+        assert bool((out[:, :16] == float("inf")).all()) and bool((out[:, 16:] == float("-inf")).all())
