@@ -386,6 +386,8 @@ hq_status hq_linear_w4_dgrad(hq_handle* h, const hq_matrix* dy, const hq_w4* w, 
  *   to even, of the exact quotient, and at most 127 in magnitude (a scale below 2^-142 has so few bits that the quotient can pass
  *   that); a group of zeros, or of values so small that the scale rounds to 0, has scale 0 and q = 0.  A group that holds an
  *   infinity or a NaN has scale NaN and q = 0: all of it is restored as NaN.
+ * f and f' are evaluated in 32 bits, to 2^-19 of |x| and to 2^-15 of the result in the tails (values of f below 2^-126, of f' below 2^-123,
+ * may become 0).
  * x, gate, y: (rows, cols) of one type, HQ_F32, HQ_F16 or HQ_BF16.  gate (and with it saved_gate) may be NULL, y may be NULL
  * (x is saved and nothing else).
  */
@@ -393,7 +395,7 @@ hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, 
                        hq_saved8* saved_x, hq_saved8* saved_gate, void* stream);
 
 /* Backward pass of hq_act_save8 from what it saved, x^ and gate^ the restored values:
- *   dx = dy * f'(x^), or dx = dy * gate^ * f'(x^) and dgate = dy * f(x^).   f' of ReLU is 0 at 0.
+ *   dx = dy * f'(x^), or dx = dy * gate^ * f'(x^) and dgate = dy * f(x^).   f' of ReLU is 0 at 0 and at NaN.
  * dy, dx, dgate: (rows, cols) of one type.  saved_gate and dgate are both given or both NULL. */
 hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act,
                            hq_matrix* dx, hq_matrix* dgate, void* stream);

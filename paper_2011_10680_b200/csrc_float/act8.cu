@@ -73,15 +73,15 @@ __device__ __forceinline__ void store8(T* dst, int n, const Two (&pairs)[kPairs]
   }
 }
 
-// (Results below 2^-126 become zero; the forms that keep them cost several instructions more.)
+// (What would be below 2^-126 becomes zero, the reciprocal of a number above 2^126 too; the forms that keep them cost several
+// instructions more.  Where that would lose a result, see far_tail.)
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float reciprocal_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// Phi(x) and exp(-x^2 / 2).  With a = |x|, Phi(-a) exp(a^2 / 2) is smooth and falls as 1 / a: a polynomial of degree eight in
-// t = 1 / (1 + 0.3 a), without a constant term, holds it to 1.4e-7 of its value for a <= 14 (least largest relative error, found
-// by linear programming), 5e-7 in 32-bit arithmetic.  So the tail keeps its relative accuracy, and the exponential serves the
-// derivative too.
-__device__ __forceinline__ Two normal_cdf(Two x, Two& bell) {
+// Phi(-a) exp(a^2 / 2) for a = |x| is smooth and falls as 1 / a: a polynomial of degree eight in t = 1 / (1 + 0.3 a), without a
+// constant term, holds it to 1.4e-7 of its value for a <= 14 (least largest relative error, found by linear programming), 5e-7 in
+// 32-bit arithmetic.
+__device__ __forceinline__ Two tail_ratio(Two x) {
   const Two a = {x.v & 0x7fffffff7fffffffull}, d = fma(both(0.3f), a, both(1.f));
   const Two t = two(reciprocal_fast(lo(d)), reciprocal_fast(hi(d)));
   Two m = both(0.0355620074f);
@@ -92,15 +92,21 @@ __device__ __forceinline__ Two normal_cdf(Two x, Two& bell) {
   m = fma(m, t, both(0.099989319f));
   m = fma(m, t, both(0.120743002f));
   m = fma(m, t, both(0.119629944f));
-  const Two e = mul(mul(x, x), both(-0.7213475204f));              // log2(e) / 2
+  return mul(m, t);
+}
+// Phi(x) and exp(-x^2 / 2): the tail keeps its relative accuracy, and the exponential serves the derivative too.
+constexpr float kBellExponent = -0.7213475204f;                     // log2(e) / 2
+__device__ __forceinline__ Two normal_cdf(Two x, Two& bell) {
+  const Two e = mul(mul(x, x), both(kBellExponent));
   bell = two(exp2_fast(lo(e)), exp2_fast(hi(e)));
-  const Two tail = mul(mul(m, t), bell), rest = fma(both(-1.f), tail, both(1.f));
+  const Two tail = mul(tail_ratio(x), bell), rest = fma(both(-1.f), tail, both(1.f));
   return two(lo(x) > 0.f ? lo(rest) : lo(tail), hi(x) > 0.f ? hi(rest) : hi(tail));
 }
 __device__ __forceinline__ Two logistic(Two x) {
   const Two e = mul(x, both(-1.4426950409f)), d = add(two(exp2_fast(lo(e)), exp2_fast(hi(e))), both(1.f));
   return two(reciprocal_fast(lo(d)), reciprocal_fast(hi(d)));
 }
+constexpr float kPhiSlope = 0.3989422804f;                          // 1 / sqrt(2 pi)
 
 // f(x) and f'(x) (what is not used of them is not computed)
 template <int ACT>
@@ -112,7 +118,7 @@ __device__ __forceinline__ Two f_and_slope(Two x, Two& slope) {
   if (ACT == HQ_ACT_GELU) {
     Two bell;
     const Two phi = normal_cdf(x, bell);
-    slope = fma(mul(x, both(0.3989422804f)), bell, phi);
+    slope = fma(mul(x, both(kPhiSlope)), bell, phi);
     return mul(x, phi);
   }
   if (ACT == HQ_ACT_SILU) {
@@ -122,6 +128,16 @@ __device__ __forceinline__ Two f_and_slope(Two x, Two& slope) {
   }
   slope = both(1.f);
   return x;
+}
+
+// SiLU far to the left is x exp(x), a normal number down to x = -91.9, while the logistic function leaves the 32-bit range at -87.3.  From
+// kFarFrom on the exponential is multiplied in as a square.  (GELU loses nothing above 2^-126 itself, and of its derivative what is
+// below 2^-123.)
+constexpr float kFarFrom = 87.f;
+__device__ __forceinline__ float silu_far(float x, float& slope) {
+  const float h = exp2_fast(x * 0.7213475204f), f = x * h * h;      // exp(x / 2)
+  slope = fmaf(h, h, f);
+  return f;
 }
 
 // Scale of a group from its largest magnitude, given as the bits of a non-negative float: in that order NaN > infinity > any
@@ -217,8 +233,9 @@ template <> __device__ __forceinline__ unsigned largest<__nv_bfloat16>(const Raw
 }
 
 // Quantizes the eight values held by each lane of a group and stores integers and scale.  Every lane of the warp takes part.
+// Returns the group's largest magnitude, as the bits of a float.
 template <class T, bool VEC>
-__device__ __forceinline__ void save_group(const Raw<T>& raw, const Two (&v)[kPairs], int lanes, int lane_in_group, int8_t* q, float* scale, int n) {
+__device__ __forceinline__ unsigned save_group(const Raw<T>& raw, const Two (&v)[kPairs], int lanes, int lane_in_group, int8_t* q, float* scale, int n) {
   unsigned top = largest<T>(raw);
   for (int d = 1; d < lanes; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
   const float s = group_scale(top);
@@ -230,6 +247,7 @@ __device__ __forceinline__ void save_group(const Raw<T>& raw, const Two (&v)[kPa
     for (int i = 0; i < kVec; ++i) if (i < n) q[i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
   }
   if (lane_in_group == 0 && n > 0) *scale = s;
+  return top;
 }
 
 __device__ __forceinline__ void restore8(uint2 w, float s, Two (&v)[kPairs]) {
@@ -263,9 +281,40 @@ __device__ __forceinline__ Slot slot_of(long long slot, const Slots& s, int cols
   return at;
 }
 
+// SiLU's far values among those of the calling thread, once more.  (By a walk of its own: whatever it needed of the kernel's would be kept in
+// registers throughout.)
+template <class T, bool GATE, int PIECES>
+__device__ __noinline__ void far_forward(const ActArgs& p, const Slots& slots) {
+  const Slot at = slot_of((long long)blockIdx.x * kThreads + threadIdx.x, slots, p.cols);
+  for (long long row = at.row; row < p.rows && row < at.row + PIECES * slots.step; row += slots.step) {
+    for (int col = at.col; col < at.col + at.n; ++col) {
+      const float x = hq_to_float(((const T*)p.x)[row * p.x_stride + col]);
+      if (!(x < -kFarFrom)) continue;
+      float slope;
+      const float f = silu_far(x, slope);
+      ((T*)p.y)[row * p.y_stride + col] = hq_from_float<T>(GATE ? f * hq_to_float(((const T*)p.gate)[row * p.gate_stride + col]) : f);
+    }
+  }
+}
+template <class T, bool GATE, int PIECES>
+__device__ __noinline__ void far_backward(const ActArgs& p, const Slots& slots) {
+  const Slot at = slot_of((long long)blockIdx.x * kThreads + threadIdx.x, slots, p.cols);
+  for (long long row = at.row; row < p.rows && row < at.row + PIECES * slots.step; row += slots.step) {
+    for (int col = at.col; col < at.col + at.n; ++col) {
+      const long long flat = row * p.cols + col, group = row * p.groups + col / p.group;
+      const float x = (float)p.xq[flat] * p.xs[group], dy = hq_to_float(((const T*)p.x)[row * p.x_stride + col]);
+      if (!(x < -kFarFrom)) continue;
+      float slope;
+      const float f = silu_far(x, slope);
+      if (GATE) ((T*)p.dgate)[row * p.dgate_stride + col] = hq_from_float<T>(dy * f);
+      ((T*)p.y)[row * p.y_stride + col] = hq_from_float<T>(GATE ? dy * ((float)p.gq[flat] * p.gs[group]) * slope : dy * slope);
+    }
+  }
+}
+
 // GATE: a second tensor.
 template <class T, int ACT, bool VEC, bool GATE, int PIECES>
-__global__ void __launch_bounds__(kThreads, 4) act_save8_kernel(const ActArgs p, const Slots slots) {
+__global__ void __launch_bounds__(kThreads, 4) act_save8_kernel(const __grid_constant__ ActArgs p, const __grid_constant__ Slots slots) {
   hq_pdl_entry();
   const int lanes = p.group / kVec, group_log = 31 - __clz(p.group);
   const int lane_in_group = threadIdx.x & (lanes - 1);
@@ -282,11 +331,12 @@ __global__ void __launch_bounds__(kThreads, 4) act_save8_kernel(const ActArgs p,
     fetch8<T, VEC>(x_at + i * slots.step * p.x_stride, n[i], raw_x[i]);
     if (GATE) fetch8<T, VEC>(g_at + i * slots.step * p.gate_stride, n[i], raw_g[GATE ? i : 0]);
   }
+  bool far = false;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     Two x[kPairs], g[kPairs];
     expand8<T>(raw_x[i], x);
-    save_group<T, VEC>(raw_x[i], x, lanes, lane_in_group, p.xq + flat, p.xs + group_at, n[i]);
+    const unsigned top = save_group<T, VEC>(raw_x[i], x, lanes, lane_in_group, p.xq + flat, p.xs + group_at, n[i]);
     if (GATE) {
       expand8<T>(raw_g[GATE ? i : 0], g);
       save_group<T, VEC>(raw_g[GATE ? i : 0], g, lanes, lane_in_group, p.gq + flat, p.gs + group_at, n[i]);
@@ -299,14 +349,16 @@ __global__ void __launch_bounds__(kThreads, 4) act_save8_kernel(const ActArgs p,
         if (GATE) x[k] = mul(x[k], g[k]);
       }
       store8<T, VEC>(y_at + i * slots.step * p.y_stride, n[i], x);
+      far = far || top >= __float_as_uint(kFarFrom);
     }
     flat += slots.step * p.cols;
     group_at += slots.step * p.groups;
   }
+  if (ACT == HQ_ACT_SILU && far) far_forward<T, GATE, PIECES>(p, slots);
 }
 
 template <class T, int ACT, bool VEC, bool GATE, int PIECES>
-__global__ void __launch_bounds__(kThreads, GATE ? 5 : 4) act_backward8_kernel(const ActArgs p, const Slots slots) {
+__global__ void __launch_bounds__(kThreads, GATE ? 5 : 4) act_backward8_kernel(const __grid_constant__ ActArgs p, const __grid_constant__ Slots slots) {
   hq_pdl_entry();
   const int group_log = 31 - __clz(p.group);
   const Slot at = slot_of((long long)blockIdx.x * kThreads + threadIdx.x, slots, p.cols);
@@ -329,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, GATE ? 5 : 4) act_backward8_kernel(c
       gs[GATE ? i : 0] = n[i] ? p.gs[group_at + i * slots.step * p.groups] : 0.f;
     }
   }
+  bool far = false;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     if (n[i] == 0) continue;
@@ -345,7 +398,9 @@ __global__ void __launch_bounds__(kThreads, GATE ? 5 : 4) act_backward8_kernel(c
     }
     if (GATE) store8<T, VEC>(dgate_at + i * slots.step * p.dgate_stride, n[i], dgate);
     store8<T, VEC>(dx_at + i * slots.step * p.y_stride, n[i], dy);
+    far = far || xs[i] * 128.f >= kFarFrom;
   }
+  if (ACT == HQ_ACT_SILU && far) far_backward<T, GATE, PIECES>(p, slots);
 }
 
 // Whole 16-byte pieces everywhere: pitches that keep every row on its 16 bytes, and whole eights of columns.

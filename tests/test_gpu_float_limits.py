@@ -117,3 +117,57 @@ def test_linear_w4_sums_beyond_32_bits_are_infinite(hq):  # noqa: F811
         assert hq.linear_w4(x, q, s, 128, None, out) == 0
         hq.sync()
         assert bool((out[:, :16] == float("inf")).all()) and bool((out[:, 16:] == float("-inf")).all())
+
+
+# ------------------------------------------------------------------------------------------------ far tails
+# Exponents of up to 130 (in base two) are products in 32 bits: off by 2.5 * 130 * ln(2) * 2^-24 of the result, and a few roundings.
+TAIL = 2.0 ** -15
+
+
+def check_tail(got, ref, dtype):
+    """Relative wherever the result is a normal number; half a unit of the subnormal ones of the type (an intermediate rounds there too)."""
+    err, unit = (got.double() - ref).abs(), torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    bound = (TAIL + 1.01 * ops.u(dtype)) * ref.abs() + 1.01 * unit
+    assert bool((err <= bound).all()), float((err / bound).max())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("cols", [4096, 4093])
+def test_silu_far_to_the_left(hq, dtype, gated, cols):  # noqa: F811
+    """x e^x is a normal 32-bit number down to x = -91.9, where e^x itself is not."""
+    x = torch.linspace(-91.5, -80.0, cols, device="cuda", dtype=torch.float64)[None].to(dtype).repeat(3, 1)
+    x[1] = x[1].flip(0)
+    x[2, ::2] = 3.0
+    gate = normal(gen(41), 3, cols).abs().add(1).to(dtype) if gated else None
+    y, (xq, xs), (gq, gs) = out_matrix(3, cols, dtype), ops.saved_pair(3, cols, 128), ops.saved_pair(3, cols, 128)
+    assert hq.act_save8(x, gate, "silu", 128, y, xq, xs, *((gq, gs) if gated else ())) == 0
+    hq.sync()
+    f = ops.f_df("silu", x.double())[0]
+    check_tail(y, f * gate.double() if gated else f, dtype)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("act,left,right", [("silu", -91.0, -60.0), ("gelu", -13.2, -10.0)])
+def test_slopes_far_to_the_left(hq, act, left, right, dtype, gated):  # noqa: F811
+    """From saved values of every magnitude in that range: one group of 32 per scale."""
+    rows, cols = 96, 32
+    xs = (torch.linspace(-left, -right, rows, device="cuda", dtype=torch.float64) / 127).float()[:, None].contiguous()
+    xq = torch.arange(127, 127 - cols, -1, device="cuda").neg().to(torch.int8).repeat(rows, 1).contiguous()
+    xq[:, 5], xq[:, 9] = 127, 0
+    gq, gs = torch.full_like(xq, 127), torch.full_like(xs, 2.0 / 127)
+    dy, dx, dgate = torch.full((rows, cols), 1.5, device="cuda", dtype=dtype), out_matrix(rows, cols, dtype), out_matrix(rows, cols, dtype)
+    if gated:
+        assert hq.act_backward8(dy, xq, xs, gq, gs, act, 32, dx, dgate) == 0
+    else:
+        assert hq.act_backward8(dy, xq, xs, None, None, act, 32, dx) == 0
+    hq.sync()
+    kept = xq.double() * xs.double()
+    f, df = ops.f_df(act, kept)
+    df_scale = 127 * gs.double() if gated else 1.0
+    keep = df.abs() > 1e-3 * ops.f_df(act, kept + 0.01)[1].abs()            # (none lies next to a zero of the derivative)
+    assert bool(keep.all())
+    check_tail(dx, 1.5 * df * df_scale, dtype)
+    if gated:
+        check_tail(dgate, 1.5 * f, dtype)
