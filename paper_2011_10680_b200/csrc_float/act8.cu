@@ -1,6 +1,6 @@
 // Activation functions whose input is saved in 8 bits (hq_act_save8), and their backward pass from what was saved
-// (hq_act_backward8).  Both are one pass over the data and bound by it: a thread holds eight neighbouring values of a row (two such
-// pieces where only one tensor is read, to keep enough bytes in flight), a group is held by group / 8 neighbouring lanes of one
+// (hq_act_backward8).  Both are one pass over the data and bound by it: a thread holds eight neighbouring values of a row (of two rows,
+// or four where one 16-bit tensor is read, to keep enough bytes in flight), a group is held by group / 8 neighbouring lanes of one
 // warp, which agree on its largest magnitude by shuffles.  At the memory's rate a value of a gated 16-bit pass has about 40
 // instruction slots, so the functions are made of the hardware's exponential and reciprocal, and an 8-bit integer of a 16-bit
 // value is one multiply-add.
@@ -417,7 +417,7 @@ cudaError_t launch_pieces(const ActArgs& a, cudaStream_t s) {
   slots.per_row = a.groups * (a.group / kVec);
   slots.step = (a.rows + kPieces - 1) / kPieces;
   slots.all = slots.step * slots.per_row;
-  slots.mul = slots.per_row == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / (unsigned)slots.per_row);
+  slots.mul = (uint32_t)((1ull << 32) / (unsigned)slots.per_row);     // (a group has four slots at least)
   const long long blocks = (slots.all + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
   const dim3 grid((unsigned)blocks), block(kThreads);
@@ -431,7 +431,7 @@ template <bool SAVE, class T, int ACT, bool VEC, bool GATE>
 cudaError_t launch_pieces(const ActArgs& a, cudaStream_t s) {
   constexpr int kPieces = !VEC ? 1 : GATE || sizeof(T) == 4 ? 2 : 4;
   const long long slots = a.rows * a.groups * (a.group / kVec);
-  if (slots < 148ll * 512 * kPieces) return launch_pieces<SAVE, T, ACT, VEC, GATE, 1>(a, s);
+  if (slots < a.sm_count * 512ll * kPieces) return launch_pieces<SAVE, T, ACT, VEC, GATE, 1>(a, s);
   return launch_pieces<SAVE, T, ACT, VEC, GATE, kPieces>(a, s);
 }
 template <bool SAVE, class T, int ACT>

@@ -76,7 +76,7 @@ hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a
 }
 
 // What hq_act_save8 and hq_act_backward8 share.
-hq_status act_args(const hq_matrix* shape, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act, ActArgs& a) {
+hq_status act_args(const hq_handle* h, const hq_matrix* shape, const hq_saved8* saved_x, const hq_saved8* saved_gate, int32_t act, ActArgs& a) {
   if (act < HQ_ACT_NONE || act > HQ_ACT_SILU) return HQ_ERR_INVALID_ARG;
   hq_status st = check_saved(saved_x, shape->rows, shape->cols);
   if (st != HQ_OK) return st;
@@ -88,7 +88,7 @@ hq_status act_args(const hq_matrix* shape, const hq_saved8* saved_x, const hq_sa
   }
   a.xq = saved_x->q; a.xs = saved_x->scale;
   a.rows = shape->rows; a.cols = (int32_t)shape->cols; a.group = saved_x->group; a.groups = groups_of(shape->cols, saved_x->group);
-  a.act = act;
+  a.act = act; a.sm_count = h->sm_count;
   return HQ_OK;
 }
 
@@ -167,7 +167,7 @@ hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, 
   if (st != HQ_OK) return st;
   if ((gate && !same_shape(x, gate)) || (y && !same_shape(x, y))) return HQ_ERR_INVALID_ARG;
   ActArgs a{};
-  st = act_args(x, saved_x, saved_gate, act, a);
+  st = act_args(h, x, saved_x, saved_gate, act, a);
   if (st != HQ_OK || x->rows == 0) return st;
   a.x = x->data; a.x_stride = x->row_stride;
   if (gate) { a.gate = gate->data; a.gate_stride = gate->row_stride; }
@@ -186,7 +186,7 @@ hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
   if (st != HQ_OK) return st;
   if (!same_shape(dy, dx) || (dgate && !same_shape(dy, dgate))) return HQ_ERR_INVALID_ARG;
   ActArgs a{};
-  st = act_args(dy, saved_x, saved_gate, act, a);
+  st = act_args(h, dy, saved_x, saved_gate, act, a);
   if (st != HQ_OK || dy->rows == 0) return st;
   a.x = dy->data; a.x_stride = dy->row_stride; a.y = dx->data; a.y_stride = dx->row_stride;
   if (dgate) { a.dgate = dgate->data; a.dgate_stride = dgate->row_stride; }

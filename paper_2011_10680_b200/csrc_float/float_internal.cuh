@@ -38,6 +38,7 @@ struct ActArgs {
   int8_t* gq; float* gs;                    // saved gate, or NULL
   long long rows; int32_t cols, group, groups;
   int32_t act;
+  int32_t sm_count;
 };
 
 __device__ __forceinline__ float hq_to_float(float v) { return v; }

@@ -96,3 +96,12 @@ def test_plan_refuses_what_it_cannot_plan():
     assert L.hq_linear_plan(0, 1, 8, 32, 32, 148, None) == binding.HQ_ERR_INVALID_ARG
     assert binding.linear_plan("dgrad", 10, 33, 64, 32)["kernel"] == "cuda_cores"
     assert binding.linear_plan("linear", 1, 4096, 4096, 128)["kernel"] == "few_rows"
+
+
+def test_launchers_take_the_number_of_sms_from_the_handle():
+    import os
+    import re
+    for name in sorted(os.listdir(build.CSRC_FLOAT)):
+        with open(os.path.join(build.CSRC_FLOAT, name)) as f:
+            code = re.sub(r"//[^\n]*", "", f.read())
+        assert not re.search(r"\b148(ll|u|ull)?\b", code), name
