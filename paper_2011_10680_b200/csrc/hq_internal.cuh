@@ -193,7 +193,7 @@ cudaError_t hq_launch_widen_weights(const void* wgt, long long values, void* out
 // Bytes holding 4-bit values (one per byte) -> packed 4-bit tensor; `values` a multiple of 8.
 cudaError_t hq_launch_expire_wait(uint32_t* status, int budget_ms, cudaStream_t s);
 cudaError_t hq_launch_pack4(const void* in, long long values, void* out, int sm_count, cudaStream_t s);
-// The products of the operators on floating-point activations (csrc_float/): what their kernels need, from hq_create.
+// The products of the operators on floating-point activations (csrc_float/): the driver's entry points that they need, from hq_create.
 bool hq_product_tc_init();
 bool hq_product_few_init();
 // Grow the handle's scratch buffer (not allowed while `s` is capturing).

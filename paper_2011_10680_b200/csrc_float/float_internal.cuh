@@ -65,15 +65,15 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
 bool hq_plan_product_few(const ProductArgs& a, int sm_count, hq_product_plan* plan);
 bool hq_plan_product_tc(ProductKind kind, const ProductArgs& a, int sm_count, hq_product_plan* plan);
 cudaError_t hq_launch_product_any(ProductKind kind, int type, const ProductArgs& a, cudaStream_t s);
-// Runs `set` the first time for the current device (its kernels' attributes stay set); again after a failure.
-template <class Set>
-inline bool hq_once_per_device(std::atomic<bool> (&done)[64], Set set) {
-  int device = 0;
-  if (cudaGetDevice(&device) != cudaSuccess) return false;
-  if (device < 64 && done[device].load()) return true;
-  if (!set()) return false;
-  if (device < 64) done[device].store(true);
-  return true;
+// Lets a kernel have that much dynamic shared memory: at its first launch on a device (`done` is the kernel's own), not when a handle is
+// made, so that a program pays for the kernels that it uses and depends on no others.  Allowed while a stream is capturing.
+constexpr int kMaxDevices = 64;
+template <class Kernel>
+inline cudaError_t hq_allow_shared(std::atomic<bool> (&done)[kMaxDevices], int device, Kernel kernel, int bytes) {
+  if (device < kMaxDevices && done[device].load()) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && device < kMaxDevices) done[device].store(true);
+  return e;
 }
 cudaError_t hq_launch_act_save8(int type, const ActArgs& a, cudaStream_t s);
 cudaError_t hq_launch_act_backward8(int type, const ActArgs& a, cudaStream_t s);

@@ -444,7 +444,10 @@ int columns_eights(int j, int parts) { return j * parts <= 8 ? 1 : 2; }
 int parts_of(const ProductArgs& a) { return a.group >= a.r || a.group % 128 == 0 ? 1 : a.group % 64 == 0 ? 2 : 4; }
 
 template <class T, int NB, int RT, bool WHOLE>
-cudaError_t launch(const CUtensorMap& map, const FewArgs& a, int grid, int shared, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap& map, const FewArgs& a, int grid, int shared, int device, cudaStream_t s) {
+  static std::atomic<bool> done[kMaxDevices];
+  const cudaError_t ready = hq_allow_shared(done, device, product_few_kernel<T, NB, RT, WHOLE>, kMaxShared);
+  if (ready != cudaSuccess) return ready;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -456,25 +459,14 @@ cudaError_t launch(const CUtensorMap& map, const FewArgs& a, int grid, int share
   return cudaLaunchKernelEx(&cfg, product_few_kernel<T, NB, RT, WHOLE>, map, a);
 }
 template <class T, bool WHOLE>
-cudaError_t launch_shape(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, cudaStream_t s) {
-  if (rt == 2) return nb == 1 ? launch<T, 1, 2, WHOLE>(map, a, grid, shared, s) : launch<T, 2, 2, WHOLE>(map, a, grid, shared, s);
-  return nb == 1 ? launch<T, 1, 1, WHOLE>(map, a, grid, shared, s) : launch<T, 2, 1, WHOLE>(map, a, grid, shared, s);
+cudaError_t launch_shape(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, int device, cudaStream_t s) {
+  if (rt == 2) return nb == 1 ? launch<T, 1, 2, WHOLE>(map, a, grid, shared, device, s) : launch<T, 2, 2, WHOLE>(map, a, grid, shared, device, s);
+  return nb == 1 ? launch<T, 1, 1, WHOLE>(map, a, grid, shared, device, s) : launch<T, 2, 1, WHOLE>(map, a, grid, shared, device, s);
 }
 template <class T>
-cudaError_t launch_type(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, cudaStream_t s) {
-  return a.parts_log == 0 ? launch_shape<T, true>(nb, rt, map, a, grid, shared, s) : launch_shape<T, false>(nb, rt, map, a, grid, shared, s);
+cudaError_t launch_type(int nb, int rt, const CUtensorMap& map, const FewArgs& a, int grid, int shared, int device, cudaStream_t s) {
+  return a.parts_log == 0 ? launch_shape<T, true>(nb, rt, map, a, grid, shared, device, s) : launch_shape<T, false>(nb, rt, map, a, grid, shared, device, s);
 }
-
-template <class T, int NB, int RT, bool WHOLE>
-bool allow_shared() {
-  return cudaFuncSetAttribute(product_few_kernel<T, NB, RT, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared) == cudaSuccess;
-}
-template <class T, bool WHOLE>
-bool allow_shapes() {
-  return allow_shared<T, 1, 1, WHOLE>() && allow_shared<T, 2, 1, WHOLE>() && allow_shared<T, 1, 2, WHOLE>() && allow_shared<T, 2, 2, WHOLE>();
-}
-template <class T>
-bool allow_type() { return allow_shapes<T, false>() && allow_shapes<T, true>(); }
 
 // The launch of a shape: sixteens of outputs per tile, cluster size, warps of a team, shared memory; false when x does not fit the
 // CTAs of a cluster.
@@ -532,10 +524,8 @@ bool plan(const ProductArgs& p, int sm_count, FewArgs& a, int& rt, int& shared) 
 
 }  // namespace
 
-bool hq_product_few_init() {
-  static std::atomic<bool> done[64];
-  return load_driver_entry_points() && hq_once_per_device(done, [] { return allow_type<__half>() && allow_type<__nv_bfloat16>(); });
-}
+// From hq_create.
+bool hq_product_few_init() { return load_driver_entry_points(); }
 
 bool hq_product_few_supported(const ProductArgs& p, int sm_count) {
   if (p.j > kMaxColumns || p.j * parts_of(p) > kMaxColumns || p.q_cols % 32 || (p.b_stride % 8 && p.j > 1)) return false;
@@ -567,6 +557,6 @@ hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& p, cu
   const int grid = (a.tiles < at_once ? a.tiles : at_once) * a.splits;
   CUtensorMap map;
   if (!encode_rows_map(&map, p.q, p.i, p.q_cols >> 1, 128, kRows * rt, CU_TENSOR_MAP_SWIZZLE_128B)) return HQ_ERR_CUDA;
-  const cudaError_t e = type == HQ_F16 ? launch_type<__half>(nb, rt, map, a, grid, shared, s) : launch_type<__nv_bfloat16>(nb, rt, map, a, grid, shared, s);
+  const cudaError_t e = type == HQ_F16 ? launch_type<__half>(nb, rt, map, a, grid, shared, h->device, s) : launch_type<__nv_bfloat16>(nb, rt, map, a, grid, shared, h->device, s);
   return e == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }

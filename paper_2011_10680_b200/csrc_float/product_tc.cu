@@ -558,7 +558,10 @@ bool encode_b_map(CUtensorMap* map, int type, const ProductArgs& a, ProductKind 
 }
 
 template <int KIND, class T, int NT>
-cudaError_t launch(const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap* map, const TcArgs& a, int grid, int device, cudaStream_t s) {
+  static std::atomic<bool> done[kMaxDevices];
+  const cudaError_t ready = hq_allow_shared(done, device, product_tc_kernel<KIND, T, NT>, Shape<KIND, NT>::kSharedBytes);
+  if (ready != cudaSuccess) return ready;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -570,36 +573,24 @@ cudaError_t launch(const CUtensorMap* map, const TcArgs& a, int grid, cudaStream
   return cudaLaunchKernelEx(&cfg, product_tc_kernel<KIND, T, NT>, map[0], map[1], a);
 }
 template <int KIND, class T>
-cudaError_t launch_width(int nt, const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
+cudaError_t launch_width(int nt, const CUtensorMap* map, const TcArgs& a, int grid, int device, cudaStream_t s) {
   switch (nt) {
-    case 32: return launch<KIND, T, 32>(map, a, grid, s);
-    case 64: return launch<KIND, T, 64>(map, a, grid, s);
-    case 128: return launch<KIND, T, 128>(map, a, grid, s);
-    default: return launch<KIND, T, 256>(map, a, grid, s);
+    case 32: return launch<KIND, T, 32>(map, a, grid, device, s);
+    case 64: return launch<KIND, T, 64>(map, a, grid, device, s);
+    case 128: return launch<KIND, T, 128>(map, a, grid, device, s);
+    default: return launch<KIND, T, 256>(map, a, grid, device, s);
   }
 }
 template <class T>
-cudaError_t launch_kind(ProductKind kind, int nt, const CUtensorMap* map, const TcArgs& a, int grid, cudaStream_t s) {
-  return kind == PRODUCT_FORWARD ? launch_width<PRODUCT_FORWARD, T>(nt, map, a, grid, s)
-       : kind == PRODUCT_DGRAD ? launch_width<PRODUCT_DGRAD, T>(nt, map, a, grid, s) : launch_width<PRODUCT_WGRAD, T>(nt, map, a, grid, s);
+cudaError_t launch_kind(ProductKind kind, int nt, const CUtensorMap* map, const TcArgs& a, int grid, int device, cudaStream_t s) {
+  return kind == PRODUCT_FORWARD ? launch_width<PRODUCT_FORWARD, T>(nt, map, a, grid, device, s)
+       : kind == PRODUCT_DGRAD ? launch_width<PRODUCT_DGRAD, T>(nt, map, a, grid, device, s) : launch_width<PRODUCT_WGRAD, T>(nt, map, a, grid, device, s);
 }
-
-template <int KIND, class T, int NT>
-bool allow_shared() {
-  return cudaFuncSetAttribute(product_tc_kernel<KIND, T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<KIND, NT>::kSharedBytes) == cudaSuccess;
-}
-template <int KIND, class T>
-bool allow_widths() { return allow_shared<KIND, T, 32>() && allow_shared<KIND, T, 64>() && allow_shared<KIND, T, 128>() && allow_shared<KIND, T, 256>(); }
-template <class T>
-bool allow_kinds() { return allow_widths<PRODUCT_FORWARD, T>() && allow_widths<PRODUCT_DGRAD, T>() && allow_widths<PRODUCT_WGRAD, T>(); }
 
 }  // namespace
 
 // From hq_create.
-bool hq_product_tc_init() {
-  static std::atomic<bool> done[64];
-  return load_driver_entry_points() && hq_once_per_device(done, [] { return allow_kinds<__half>() && allow_kinds<__nv_bfloat16>(); });
-}
+bool hq_product_tc_init() { return load_driver_entry_points(); }
 
 bool hq_product_tc_supported(ProductKind kind, const ProductArgs& a) {
   if (a.r < 1) return false;
@@ -681,6 +672,6 @@ hq_status hq_launch_product_tc(hq_handle* h, ProductKind kind, int type, const P
   const int unit_rows = kind == PRODUCT_FORWARD ? kTileC : kStep;
   if (!encode_rows_map(&map[0], p.q, kind == PRODUCT_FORWARD ? p.i : p.r, bytes ? p.q_cols : p.q_cols >> 1, unit_row, unit_rows, swizzle_for(unit_row)) ||
       !encode_b_map(&map[1], type, p, kind, nt)) return HQ_ERR_CUDA;
-  const cudaError_t e = type == HQ_F16 ? launch_kind<__half>(kind, nt, map, a, grid, s) : launch_kind<__nv_bfloat16>(kind, nt, map, a, grid, s);
+  const cudaError_t e = type == HQ_F16 ? launch_kind<__half>(kind, nt, map, a, grid, h->device, s) : launch_kind<__nv_bfloat16>(kind, nt, map, a, grid, h->device, s);
   return e == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }
