@@ -327,7 +327,8 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
  *
  *   - matrices are row-major with a stride between rows; `data`, the quantized arrays and their scales are
  *     16-byte aligned (HQ_ERR_ALIGNMENT), biases aligned to their type;
- *   - every call runs on the device of its handle, whatever the current one; `stream` belongs to that device;
+ *   - every call runs on the device of its handle, whatever the thread's current device or context, and leaves that current;
+ *     `stream` belongs to the handle's device (to its primary context);
  *   - input and output of a call must not overlap; rows x cols of a matrix may be as large as memory allows,
  *     neither of them above 2^30 (HQ_ERR_UNSUPPORTED); rows == 0 is allowed;
  *   - no call allocates or needs scratch memory: calls through one handle may run on several streams at once,

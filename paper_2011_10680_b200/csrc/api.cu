@@ -378,7 +378,7 @@ hq_status hq_create(int32_t device, hq_handle** out) {
   h->sm_count = prop.multiProcessorCount;
   h->workspace = nullptr;
   h->workspace_bytes = 0;
-  if (!hq_conv_tc_init() || !hq_conv_small_init() || !hq_product_tc_init() || !hq_product_few_init()) { delete h; return HQ_ERR_CUDA; }
+  if (!hq_conv_tc_init() || !hq_conv_small_init() || !hq_product_tc_init() || !hq_product_few_init() || !hq_float_init(h)) { delete h; return HQ_ERR_CUDA; }
   if (cudaMalloc(&h->dev_status, sizeof(uint32_t)) != cudaSuccess) { delete h; return HQ_ERR_WORKSPACE; }
   if (cudaMemset(h->dev_status, 0, sizeof(uint32_t)) != cudaSuccess) { cudaFree(h->dev_status); delete h; return HQ_ERR_CUDA; }
   if (cudaMalloc(&h->narrow_pairs, (size_t)2 * kNarrowChannels * 16) != cudaSuccess) {

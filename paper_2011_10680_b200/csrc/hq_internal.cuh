@@ -18,6 +18,7 @@ enum : uint32_t {
 
 struct hq_handle {
   int32_t device;
+  void* context;              // of that device: the operators of csrc_float/ run in it, whichever is current
   int32_t conv_path;          // see hq_set_conv_path
   int32_t sm_count;
   uint32_t* dev_status;       // one word in device memory, sticky until hq_sync
@@ -195,6 +196,7 @@ cudaError_t hq_launch_expire_wait(uint32_t* status, int budget_ms, cudaStream_t 
 cudaError_t hq_launch_pack4(const void* in, long long values, void* out, int sm_count, cudaStream_t s);
 // The products of the operators on floating-point activations (csrc_float/): the driver's entry points that they need, from hq_create.
 bool hq_product_tc_init();
+bool hq_float_init(hq_handle* h);
 bool hq_product_few_init();
 // Grow the handle's scratch buffer (not allowed while `s` is capturing).
 hq_status hq_reserve_workspace(hq_handle* h, size_t bytes, cudaStream_t s);

@@ -1,27 +1,34 @@
 // C ABI of the operators on floating-point activations: argument checks and the choice of kernel.  Host code only.
+#include <mutex>
+
+#include <cuda.h>
+
 #include "float_internal.cuh"
 
 namespace {
 
 constexpr long long kMaxExtent = 1ll << 30;     // 32-bit indexes of a tile or a group may reach past the last row or column
 
-// The handle's device for the duration of a call.  A host thread that has made no call to the runtime yet has no context, which
-// encoding a tensor map needs; cudaSetDevice gives it one.
-class DeviceScope {
+CUresult (*g_current_context)(CUcontext*) = nullptr;
+CUresult (*g_set_context)(CUcontext) = nullptr;
+
+// The context of the handle's device for the duration of a call, then again whatever the thread had: the context of another device, one
+// that the program has made itself (a stream and memory of this handle are nothing to it, although the device may be the
+// same), or none.
+class ContextScope {
  public:
-  explicit DeviceScope(int device) {
-    thread_local bool has_context = false;
-    ok_ = cudaGetDevice(&before_) == cudaSuccess && ((before_ == device && has_context) || cudaSetDevice(device) == cudaSuccess);
-    has_context = has_context || ok_;
-    changed_ = ok_ && before_ != device;
+  explicit ContextScope(const hq_handle* h) {
+    const CUcontext wanted = (CUcontext)h->context;
+    ok_ = g_current_context && g_current_context(&before_) == CUDA_SUCCESS && (before_ == wanted || g_set_context(wanted) == CUDA_SUCCESS);
+    changed_ = ok_ && before_ != wanted;
   }
-  ~DeviceScope() { if (changed_) cudaSetDevice(before_); }
-  DeviceScope(const DeviceScope&) = delete;
-  DeviceScope& operator=(const DeviceScope&) = delete;
+  ~ContextScope() { if (changed_) g_set_context(before_); }
+  ContextScope(const ContextScope&) = delete;
+  ContextScope& operator=(const ContextScope&) = delete;
   bool ok() const { return ok_; }
 
  private:
-  int before_ = 0;
+  CUcontext before_ = nullptr;
   bool ok_ = false, changed_ = false;
 };
 
@@ -65,8 +72,8 @@ inline hq_status launched(hq_status st) {
 inline int groups_of(long long cols, int group) { return (int)((cols + group - 1) / group); }
 
 hq_status product(hq_handle* h, ProductKind kind, int type, const ProductArgs& a, void* stream) {
-  const DeviceScope device(h->device);
-  if (!device.ok()) return HQ_ERR_CUDA;
+  const ContextScope context(h);
+  if (!context.ok()) return HQ_ERR_CUDA;
   if (kind == PRODUCT_FORWARD && hq_product_few_supported(a, h->sm_count)) return launched(hq_launch_product_few(h, type, a, (cudaStream_t)stream));
   if (hq_product_tc_supported(kind, a)) {
     const hq_status st = launched(hq_launch_product_tc(h, kind, type, a, (cudaStream_t)stream));
@@ -93,6 +100,24 @@ hq_status act_args(const hq_handle* h, const hq_matrix* shape, const hq_saved8* 
 }
 
 }  // namespace
+
+// From hq_create, with the handle's device current.
+bool hq_float_init(hq_handle* h) {
+  static std::mutex lock;
+  const std::lock_guard<std::mutex> held(lock);
+  void *get = nullptr, *set = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuCtxGetCurrent", &get, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess ||
+      cudaGetDriverEntryPoint("cuCtxSetCurrent", &set, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return false;
+  if (!g_current_context) {
+    g_set_context = (CUresult (*)(CUcontext))set;
+    g_current_context = (CUresult (*)(CUcontext*))get;
+  }
+  CUcontext context = nullptr;
+  if (g_current_context(&context) != CUDA_SUCCESS || !context) return false;
+  h->context = context;
+  return true;
+}
 
 extern "C" {
 
@@ -172,8 +197,8 @@ hq_status hq_act_save8(hq_handle* h, const hq_matrix* x, const hq_matrix* gate, 
   a.x = x->data; a.x_stride = x->row_stride;
   if (gate) { a.gate = gate->data; a.gate_stride = gate->row_stride; }
   if (y) { a.y = y->data; a.y_stride = y->row_stride; }
-  const DeviceScope device(h->device);
-  if (!device.ok()) return HQ_ERR_CUDA;
+  const ContextScope context(h);
+  if (!context.ok()) return HQ_ERR_CUDA;
   return launched(hq_launch_act_save8(x->type, a, (cudaStream_t)stream));
 }
 
@@ -190,8 +215,8 @@ hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
   if (st != HQ_OK || dy->rows == 0) return st;
   a.x = dy->data; a.x_stride = dy->row_stride; a.y = dx->data; a.y_stride = dx->row_stride;
   if (dgate) { a.dgate = dgate->data; a.dgate_stride = dgate->row_stride; }
-  const DeviceScope device(h->device);
-  if (!device.ok()) return HQ_ERR_CUDA;
+  const ContextScope context(h);
+  if (!context.ok()) return HQ_ERR_CUDA;
   return launched(hq_launch_act_backward8(dy->type, a, (cudaStream_t)stream));
 }
 
