@@ -235,7 +235,7 @@ _PACK_MATRIX = struct.Struct("@P3qi4x").pack
 _PACK_W4 = struct.Struct("@2P3i4x").pack
 _PACK_SAVED8 = struct.Struct("@2P2qi4x").pack
 _FLOAT_TYPES: dict = {}
-_SAVED_TYPES: list = []                      # of the integers and the scales of saved activations
+_SAVED_TYPES: tuple = ()                     # of the integers and the scales of saved activations
 
 
 def _float_types() -> dict:
@@ -244,6 +244,14 @@ def _float_types() -> dict:
         import torch
         _FLOAT_TYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
     return _FLOAT_TYPES
+
+
+def _saved_types() -> tuple:
+    global _SAVED_TYPES
+    if not _SAVED_TYPES:
+        import torch
+        _SAVED_TYPES = (torch.int8, torch.float32)
+    return _SAVED_TYPES
 
 
 def _packed_matrix(t, device: int) -> bytes:
@@ -318,9 +326,6 @@ class Handle:
     def __init__(self, device: int = 0):
         self._h = C.c_void_p()
         self.device = device
-        if not _SAVED_TYPES:
-            import torch
-            _SAVED_TYPES.extend((torch.int8, torch.float32))
         _check(lib().hq_create(device, C.byref(self._h)), "hq_create")
 
     def close(self):
@@ -413,8 +418,9 @@ class Handle:
         return _PACK_W4(q.data_ptr(), scale.data_ptr(), n, k, group)
 
     def _saved8(self, q, scale, group: int) -> bytes:
-        rows, cols = _grouped(q, scale, group, 1, _SAVED_TYPES[1], self.device)
-        if q.dtype is not _SAVED_TYPES[0]:
+        integers, scales = _SAVED_TYPES or _saved_types()
+        rows, cols = _grouped(q, scale, group, 1, scales, self.device)
+        if q.dtype is not integers:
             raise ValueError("saved activations are int8 with float32 scales")
         return _PACK_SAVED8(q.data_ptr(), scale.data_ptr(), rows, cols, group)
 
