@@ -335,7 +335,8 @@ hq_status hq_ilp_solve(int32_t n_layers, const int64_t* omega, const int64_t* si
  *     and can be captured into graphs;
  *   - products run on the tensor cores where rows start on 16 bytes: strides of 16-bit matrices a multiple of 8 (any
  *     number of columns), k of hq_w4 a multiple of 32, cols of a saved matrix a multiple of 16; other shapes take a
- *     plain and much slower kernel with the same results up to rounding;
+ *     plain and much slower kernel (tens of times, for large ones) with the same results up to rounding.  A layer whose n is no
+ *     multiple of 8 runs forward on the tensor cores; its gradients do where the rows of dy are padded to such a stride;
  *   - infinities and NaN go through the arithmetic as IEEE has them; an expired device-side wait is reported by hq_sync.
  * ===================================================================================================== */
 typedef enum { HQ_F32 = 0, HQ_F16 = 1, HQ_BF16 = 2 } hq_float_type;
@@ -372,8 +373,9 @@ typedef enum {
  * Linear layer:  out[m][i] = bias[i] + sum_j x[m][j] * w[i][j].
  * x: (m, k), out: (m, n), both HQ_F16 or HQ_BF16 and of one type; bias: n values of that type or NULL.  With few rows (one token
  * of each of a few sequences: up to 16, or 8 / 4 where two / four groups share 128 inputs, as long as they fit in shared
- * memory) the weights' integers enter the products and a group's sum is scaled in 32 bits; with more, each w[i][j] is first rounded to the type of x, as a 16-bit
- * weight matrix would hold it.
+ * memory) the weights' integers enter the products and a group's sum is scaled in 32 bits; with more, each w[i][j] is first
+ * rounded to the type of x, as a 16-bit weight matrix would hold it.  So a row's results differ by that rounding between the two, and
+ * with HQ_F16 a scale above 8188 makes infinite weights (8 times it passes 65504) with many rows only.
  */
 hq_status hq_linear_w4(hq_handle* h, const hq_matrix* x, const hq_w4* w, const void* bias, hq_matrix* out, void* stream);
 
@@ -404,7 +406,8 @@ hq_status hq_act_backward8(hq_handle* h, const hq_matrix* dy, const hq_saved8* s
 /*
  * Gradient of a weight matrix whose input was saved in 8 bits:  dw[i][j] = sum_m dy[m][i] * q[m][j] * scale[m][j / group].
  * dy: (m, n), dw: (n, k), both HQ_F16 or HQ_BF16 and of one type; saved: (m, k).  Each restored value is rounded to the type
- * of dy before the products.  m == 0 writes zeros.
+ * of dy before the products (HQ_F16: values above 65504, which activations of another type can have, become infinite).  m == 0
+ * writes zeros.
  */
 hq_status hq_linear_wgrad8(hq_handle* h, const hq_matrix* dy, const hq_saved8* saved, hq_matrix* dw, void* stream);
 

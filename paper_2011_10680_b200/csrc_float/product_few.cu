@@ -9,8 +9,10 @@
 //     the same order (weights of zero give exactly zero), and the sum over a group is scaled in 32 bits.
 //   - x is stored in shared memory once per CTA, in the order in which the nibbles come out of a word (0 4 1 5 2 6 3 7 of every
 //     eight), as 16-bit floats under a power of two per row and 128 inputs that brings the largest of them to 2^15 .. 2^16, those
-//     that meet upper nibbles divided by 16.  bf16 and fp16 values are held exactly down to 2^-26 of the largest one; below, to
-//     2^-36 of it, which is 2^-12 of what one addition in 32 bits rounds away.
+//     that meet upper nibbles divided by 16.  fp16 values are held exactly from 2^-25 of the largest one up, bf16 values from 2^-28; below,
+//     to 2^-36 of it, which is 2^-12 of what one addition in 32 bits rounds away.  The sum with u and the one it is corrected by
+//     are up to 8 sum |x|, so the 32-bit additions round to 2^-24 of that, whatever the weights: a value 2^14 times the others' size
+//     that meets a weight of zero still leaves 2^-21 of itself times the scale, some 2^-14 of a usual result.
 //   - Groups shorter than 128: the eight columns of the instruction carry a row's inputs group by group, zeros elsewhere, so that
 //     every group has a sum of its own ("parts"; 64: two columns per row, 32: four).
 //   - Few outputs: a team of 2 .. 16 warps of a CTA splits the inputs of a tile, the CTAs of a cluster do too, and the parts are
@@ -557,6 +559,7 @@ hq_status hq_launch_product_few(hq_handle* h, int type, const ProductArgs& p, cu
   const int grid = (a.tiles < at_once ? a.tiles : at_once) * a.splits;
   CUtensorMap map;
   if (!encode_rows_map(&map, p.q, p.i, p.q_cols >> 1, 128, kRows * rt, CU_TENSOR_MAP_SWIZZLE_128B)) return HQ_ERR_CUDA;
-  const cudaError_t e = type == HQ_F16 ? launch_type<__half>(nb, rt, map, a, grid, shared, h->device, s) : launch_type<__nv_bfloat16>(nb, rt, map, a, grid, shared, h->device, s);
+  const cudaError_t e = type == HQ_F16 ? launch_type<__half>(nb, rt, map, a, grid, shared, h->device, s)
+                                       : launch_type<__nv_bfloat16>(nb, rt, map, a, grid, shared, h->device, s);
   return e == cudaSuccess ? HQ_OK : HQ_ERR_CUDA;
 }

@@ -9,10 +9,12 @@
 // CTAs share their MMAs (cta_group::2).  When there are too few tiles to go round, the CTAs or pairs of a cluster share a tile's
 // reduction and add their parts in rank order through distributed shared memory.
 //
-// What bounds it.  256 columns: the tensor cores under the power cap - 4001 tokens, 16384 x 4096 bf16 in 391 us alone (1373 TFLOP/s, 0.82
-// of the measured burst, at the sustained rate), 459 us back to back; 8192 x 16384 x 4096 fp16 gradient 776 us (1416).  Few
-// columns: the converters' instructions, 17 per eight 4-bit weights and about 600 cycles a stage, and some 4 us before the first
-// MMA and behind the last - 48 tokens, 8192 x 8192: 29 us, 1.3 TB/s.
+// What bounds it.  256 columns: the tensor cores under the power cap - 4001 tokens, 16384 x 4096 bf16 in 387 us alone (1388 TFLOP/s, 0.83
+// of the measured burst, at the sustained rate), 443 us back to back; 8192 x 16384 x 4096 fp16 gradient 780 us (1410).  Few
+// columns: the turn of a stage through converters and barriers, some 600 cycles (650 with 256 columns), and some 4 us before the first
+// MMA and behind the last - 48 tokens, 8192 x 8192: 29 us, 1.4 TB/s.  Neither the memory nor the arithmetic is full then: of 1294 warp
+// instructions a stage 544 convert (17 per eight weights), 1.6 a cycle are issued of 4, and warps wait most for loaded scales and
+// at barriers.
 #include <type_traits>
 
 #include "../csrc/tc_common.cuh"
@@ -116,8 +118,11 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
       ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
-// Arrival on a barrier of the leading CTA (`bar`: cluster address).  What the arrival announces was made visible before: operands by a
-// proxy fence, tensor memory by a tcgen05 fence.  (With release semantics at cluster scope the instruction took 1200 to 1700 cycles.)
+// Arrival on a barrier of the leading CTA (`bar`: cluster address).  By the letter of the memory model what is announced to another CTA is
+// released at cluster scope; that instruction took 1200 to 1700 cycles.  This form releases at CTA scope.  What it announces was made
+// visible where it lies before - operands, which the MMA reads from their own SM, by a proxy fence, tensor memory by a tcgen05
+// fence - and a pair's arrivals are usually written like this, but that it suffices rests on observation: repeated calls of every
+// shape on pairs give the same bits, and the right ones.
 __device__ __forceinline__ void arrive_leading(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
