@@ -68,7 +68,7 @@ template <int KIND, int NT>
 struct Shape {
   static constexpr bool kPair = NT == 256, kWgrad = KIND == PRODUCT_WGRAD;
   static constexpr int kCtas = kPair ? 2 : 1, kColumnsHere = NT / kCtas;
-  static constexpr int kStages = kWgrad ? (NT >= 128 ? 5 : 6) : NT >= 128 ? 6 : 8;
+  static constexpr int kStages = kWgrad ? 5 : NT >= 128 ? 6 : 8;    // (WGRAD with 64 columns or less: six, adapter 19.7 us against 19.3)
   static constexpr int kStageBytes = kTileABytes + (kColumnsHere < 64 ? 64 : kColumnsHere) * kStep * 2;
   static constexpr int kPer = Unit<KIND, NT>::kStagesOf;
   static constexpr int kUnits = kWgrad ? 8 : kStages / kPer;       // of the ring of the quantized operand: 64 KB, 24 or 32
