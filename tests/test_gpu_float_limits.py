@@ -169,3 +169,28 @@ def test_slopes_far_to_the_left(hq, act, left, right, dtype, gated):  # noqa: F8
     check_tail(dx, 1.5 * df * df_scale, dtype)
     if gated:
         check_tail(dgate, 1.5 * f, dtype)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 2.0 ** 80, -(2.0 ** 75)])
+@pytest.mark.parametrize("at", [3, 8000, 16381])
+@pytest.mark.parametrize("m,n", [(1, 64), (2, 40), (11, 4097)])
+def test_linear_w4_large_values_anywhere_in_a_row(hq, m, n, at, bad):  # noqa: F811
+    """One value that the 16-bit form of few rows does not hold, in the inputs of any CTA that shares the row; strided output, bias."""
+    g, k, group = gen(33), 16384, 128
+    q, s, w = ops.random_w4(g, n, k, group, BF16)
+    x = normal(g, m, k).to(BF16)
+    x[m - 1, at] = bad
+    bias = normal(g, n).to(BF16)
+    out = out_matrix(m, n, BF16, n + 7)
+    assert hq.linear_w4(x, q, s, group, bias, out) == 0
+    hq.sync()
+    wx = w * x.double()[:, None, :] if m * n < 1000 else None
+    ref = (wx.sum(dim=2) if wx is not None else torch.stack([(w * r).sum(dim=1) for r in x.double()])) + bias.double()
+    magnitude = torch.stack([(w * r).abs().sum(dim=1) for r in x.double()]) + bias.double().abs()
+    assert torch.equal(torch.isnan(out), torch.isnan(ref))
+    fine = torch.isfinite(ref)
+    assert torch.equal(out[~fine & ~torch.isnan(ref)].double(), ref[~fine & ~torch.isnan(ref)])
+    # (few rows: a value above 2^73 makes all rows of the call go value by value)
+    bound = 1.01 * ops.u(BF16) * ref.abs() + (k + 16) * 2.0 ** -24 * magnitude
+    assert bool(((out.double() - ref).abs() <= bound)[fine].all())
+    assert ops.unwritten_between(out)
